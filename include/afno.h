@@ -231,6 +231,94 @@ int afno_filter_backward(const void* x, const void* w1, const void* b1, const vo
                          hipStream_t stream);
 
 /*
+ * Training around the filter: linear products, LayerNorm and dropout, each with its gradient --
+ * the rest of an AFNO block (LayerNorm, the channel MLP, the residual adds) as operators of their
+ * own.  Arrays are rows of channels, [M][C] with the channels fastest (a [B][H][W][C] grid: M = B H W),
+ * contiguous device memory on the current device, aligned to their element (16 bytes take the wider
+ * kernels).  Any M >= 0 below 2^31 and any width up to 2^20 (AFNO_ERR_UNSUPPORTED beyond).  No output
+ * may overlap an input or another output (AFNO_ERR_ALIAS).  Ownership, asynchrony and errors as
+ * afno_filter_forward; sums are held in float32 and added in a fixed order, so repeated calls give
+ * the same bits.
+ *
+ * Workspace.  afno_*_workspace gives the bytes that a call of these sizes may need (0: none; an error
+ * code for sizes that the call refuses).  With workspace non-NULL the call uses the caller's memory:
+ * at least that many bytes, 16-byte aligned, apart from every array, the call's alone until its work
+ * has ended, so that captured graphs that may run at the same time need one each.  With NULL the
+ * library takes one of its own as afno_filter_forward does, except under stream capture, where a
+ * call that needs one returns AFNO_ERR_UNSUPPORTED.
+ *
+ * Dropout.  Element e (its flat index) is kept where number e % 8 of group e / 8 is at least
+ * T = 65536 p rounded to a whole number, and scaled by 65536 / (65536 - T); else it becomes 0,
+ * whatever it was.  A group's eight 16-bit numbers are the words of Philox4x32 with seven rounds, low
+ * halves first, of the counter (group low, group high, place low, place high) with the seed as key;
+ * place = offset + *counter modulo 2^64 (counter NULL: offset).  counter is a device address that
+ * is read when the kernel runs, so that a captured training step draws anew in each replay.  The
+ * mask is a function of these numbers alone and is never stored.  0 <= p < 1, and T < 65536.
+ */
+enum { AFNO_ACT_NONE = 0, AFNO_ACT_RELU = 1, AFNO_ACT_GELU = 2 };
+
+/*
+ * afno_linear_forward -- out = drop(act(x w + b)) + residual.
+ *   x [M][K], w [K][N] (input-major: x w), b [N] or NULL, residual [M][N] or NULL    dtype
+ *   activation  none, ReLU, or the exact GELU z Phi(z)
+ *   out [M][N]           dtype; one rounding from the float32 sum
+ *   pre [M][N] or NULL   dtype: x w + b, which the gradient of an activation takes
+ * M == 0 returns AFNO_OK without touching the GPU.
+ */
+int afno_linear_forward(const void* x, const void* w, const void* b, const void* residual, int64_t M,
+                        int64_t K, int64_t N, int activation, float p, uint64_t seed,
+                        uint64_t offset, const uint64_t* counter, int dtype, void* out, void* pre,
+                        void* workspace, int64_t workspace_bytes, hipStream_t stream);
+int64_t afno_linear_forward_workspace(int64_t M, int64_t K, int64_t N, int dtype);
+
+/*
+ * afno_linear_backward -- gradients of afno_linear_forward for g = dL/dout (the residual's is g):
+ *   dz = act'(pre) drop(g);  dx = dz w^T [M][K],  dw = x^T dz [K][N],  db = sum of dz's rows [N]
+ * (relu'(0) = 0).  dx, dw and db are in dtype and overwritten; each may be NULL, at least one is not.
+ * pre is not read where the activation is none, w only for dx, x only for dw.  dz is rounded to dtype
+ * before the products; db sums the unrounded values.  M == 0: dw and db are 0.
+ */
+int afno_linear_backward(const void* g, const void* x, const void* w, const void* pre, int64_t M,
+                         int64_t K, int64_t N, int activation, float p, uint64_t seed,
+                         uint64_t offset, const uint64_t* counter, int dtype, void* dx, void* dw,
+                         void* db, void* workspace, int64_t workspace_bytes, hipStream_t stream);
+int64_t afno_linear_backward_workspace(int64_t M, int64_t K, int64_t N, int dtype);
+
+/*
+ * afno_layer_norm_forward -- v = x + residual rounded to dtype (residual NULL: v = x);
+ *   out = (v - mean) / sqrt(var + eps) * gamma + beta over the C channels of a row, biased variance.
+ *   x, residual, out [M][C], gamma, beta [C]   dtype;  eps finite and >= 0
+ *   sum [M][C] or NULL   dtype: v, the residual stream and what the gradient takes
+ */
+int afno_layer_norm_forward(const void* x, const void* residual, const void* gamma, const void* beta,
+                            int64_t M, int64_t C, float eps, int dtype, void* out, void* sum,
+                            hipStream_t stream);
+
+/*
+ * afno_layer_norm_backward -- gradients of the norm of x (the v above) for g = dL/dout:
+ *   with a = g gamma and h = (x - mean) / sqrt(var + eps):
+ *   dx = (a - mean(a) - h mean(a h)) / sqrt(var + eps) + gsum
+ *   dgamma = sum over the rows of g h,  dbeta = sum over the rows of g
+ *   gsum [M][C] or NULL  dtype: the gradient that reaches v along the residual stream
+ *   dx [M][C] dtype; dgamma, dbeta [C] float32, overwritten.  M == 0: dgamma and dbeta are 0.
+ */
+int afno_layer_norm_backward(const void* g, const void* x, const void* gamma, const void* gsum,
+                             int64_t M, int64_t C, float eps, int dtype, void* dx, float* dgamma,
+                             float* dbeta, void* workspace, int64_t workspace_bytes,
+                             hipStream_t stream);
+int64_t afno_layer_norm_backward_workspace(int64_t M, int64_t C, int dtype);
+
+/*
+ * afno_dropout_forward -- out = drop(x) + residual (NULL: none) over n elements of dtype;
+ * afno_dropout_backward -- dx = drop(g) with the same numbers (the residual's gradient is g).
+ */
+int afno_dropout_forward(const void* x, const void* residual, int64_t n, float p, uint64_t seed,
+                         uint64_t offset, const uint64_t* counter, int dtype, void* out,
+                         hipStream_t stream);
+int afno_dropout_backward(const void* g, int64_t n, float p, uint64_t seed, uint64_t offset,
+                          const uint64_t* counter, int dtype, void* dx, hipStream_t stream);
+
+/*
  * Diagnostic per-kernel timing.  afno_profile_begin(max_calls) creates HIP events for
  * up to max_calls filter calls (process-wide); each later afno_filter_forward call
  * records an event before its first kernel and after each of its four phases, on the

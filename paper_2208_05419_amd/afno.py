@@ -23,6 +23,10 @@ AFNO_STAGE_SPECTRUM = 1
 AFNO_STAGE_MIXED = 2
 AFNO_STAGE_DELTA = 3
 
+AFNO_ACT_NONE = 0
+AFNO_ACT_RELU = 1
+AFNO_ACT_GELU = 2
+
 AFNO_PATH_AUTO = 0
 AFNO_PATH_GENERIC = 1
 AFNO_PATH_VALU_DFT = 2
@@ -30,6 +34,10 @@ AFNO_PATH_VALU_DFT = 2
 EXPORTED = ("afno_filter_forward", "afno_filter_forward_noalloc", "afno_filter_forward_hidden",
             "afno_block_forward",
             "afno_filter_stage", "afno_filter_stage_hidden", "afno_filter_backward",
+            "afno_linear_forward", "afno_linear_backward", "afno_layer_norm_forward",
+            "afno_layer_norm_backward", "afno_dropout_forward", "afno_dropout_backward",
+            "afno_linear_forward_workspace", "afno_linear_backward_workspace",
+            "afno_layer_norm_backward_workspace",
             "afno_profile_begin", "afno_profile_end", "afno_set_kernel_path", "afno_last_error",
             "afno_version")
 KERNELS = ("prep", "row_r2c", "column", "row_c2r")
@@ -85,6 +93,22 @@ def load_library():
     lib.afno_filter_backward.argtypes = [vp, vp, vp, vp, vp, vp, i64, i64, i64, i64, i64, f32, f32,
                                          ctypes.c_int, vp, vp, vp, vp, vp, vp]
     lib.afno_filter_backward.restype = ctypes.c_int
+    ci, u64 = ctypes.c_int, ctypes.c_uint64
+    drop = [f32, u64, u64, vp]  # p, seed, offset, counter
+    lib.afno_linear_forward.argtypes = [vp] * 4 + [i64] * 3 + [ci] + drop + [ci] + [vp] * 3 + [i64, vp]
+    lib.afno_linear_backward.argtypes = [vp] * 4 + [i64] * 3 + [ci] + drop + [ci] + [vp] * 4 + [i64, vp]
+    lib.afno_layer_norm_forward.argtypes = [vp] * 4 + [i64, i64, f32, ci, vp, vp, vp]
+    lib.afno_layer_norm_backward.argtypes = [vp] * 4 + [i64, i64, f32, ci] + [vp] * 4 + [i64, vp]
+    lib.afno_dropout_forward.argtypes = [vp, vp, i64] + drop + [ci, vp, vp]
+    lib.afno_dropout_backward.argtypes = [vp, i64] + drop + [ci, vp, vp]
+    for name in ("linear_forward", "linear_backward", "layer_norm_forward", "layer_norm_backward",
+                 "dropout_forward", "dropout_backward"):
+        getattr(lib, "afno_" + name).restype = ci
+    lib.afno_linear_forward_workspace.argtypes = [i64, i64, i64, ci]
+    lib.afno_linear_backward_workspace.argtypes = [i64, i64, i64, ci]
+    lib.afno_layer_norm_backward_workspace.argtypes = [i64, i64, ci]
+    for name in ("linear_forward", "linear_backward", "layer_norm_backward"):
+        getattr(lib, f"afno_{name}_workspace").restype = i64
     lib.afno_last_error.argtypes = []
     lib.afno_last_error.restype = ctypes.c_char_p
     lib.afno_version.argtypes = []

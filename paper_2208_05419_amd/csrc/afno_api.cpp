@@ -588,3 +588,5 @@ const char* afno_last_error(void) { return g_last_error.c_str(); }
 int afno_version(void) { return 100; }
 
 }  // extern "C"
+
+#include "afno_api_train.h"

@@ -220,4 +220,21 @@ __device__ __forceinline__ int opq(int v) {
   return v;
 }
 
+// Sum over the 64 lanes of a wave, the same in every lane.
+__device__ __forceinline__ float wave_sum(float v) {
+#pragma unroll
+  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
+  return v;
+}
+
+// Eight bf16 of a 16-byte word as floats.
+__device__ __forceinline__ void unpack8(uint4 w, float (&v)[8]) {
+  const uint32_t* u = reinterpret_cast<const uint32_t*>(&w);
+#pragma unroll
+  for (int p = 0; p < 4; ++p) {
+    v[2 * p] = __uint_as_float(u[p] << 16);
+    v[2 * p + 1] = __uint_as_float(u[p] & 0xffff0000u);
+  }
+}
+
 }  // namespace afno

@@ -9,6 +9,7 @@
 //   h   = GELU(w Wa + ba)                 gemm_dma<kEpiGelu>, or gemm_bf16 for other shapes
 //   out = v + h Wb + bb                   gemm_dma<kEpiResidual>
 #pragma once
+#include "gelu.h"
 #include "kernel_common.h"
 #include "kernels_mfma.h"
 
@@ -16,12 +17,6 @@ namespace afno {
 
 constexpr int kLnMaxPerLane = 32;  // values a lane holds: C <= 64 * 32
 constexpr float kLnEps = 1e-6f;
-
-__device__ __forceinline__ float wave_sum(float v) {
-#pragma unroll
-  for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o, 64);
-  return v;
-}
 
 // LayerNorm of one token's C channels held as vals[0 .. n) by this lane (channels
 // 8 (lane + 64 i) .. + 7 for chunk i), two passes over registers; writes bf16.
@@ -66,15 +61,6 @@ __device__ __forceinline__ void ln_token(float (&vals)[NCH][8], int nchunk, int 
       }
       *reinterpret_cast<uint4*>(y + 8 * ch) = make_uint4(o[0], o[1], o[2], o[3]);
     }
-  }
-}
-
-__device__ __forceinline__ void unpack8(uint4 w, float (&v)[8]) {
-  const uint32_t* u = reinterpret_cast<const uint32_t*>(&w);
-#pragma unroll
-  for (int p = 0; p < 4; ++p) {
-    v[2 * p] = __uint_as_float(u[p] << 16);
-    v[2 * p + 1] = __uint_as_float(u[p] & 0xffff0000u);
   }
 }
 
@@ -176,32 +162,6 @@ __global__ void __launch_bounds__(256) add_layer_norm_kernel(const bf16* __restr
 
 enum { kEpiGelu = 0, kEpiResidual = 1 };
 typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
-
-// GELU(z) = z Phi(z).  The lower tail u = Phi(-|z|) = t Q(t) exp(-z^2 / 2), t = 1 / (1 + 0.3 |z|),
-// with Q a degree-7 fit to erfcx(|z| / sqrt 2) / (2 t) on |z| <= 9 (least squares reweighted to a
-// minimax relative error of 5e-8); then z - |z| u above zero and z u below.  Against float64 the
-// result, in single precision, is within 7e-7 of its own size for z > -3 and 7e-6 from there to
-// -12.9 (a model in float32 of every step: 4.4e-7 and 6.7e-6; the fit reaches past its 9), and within
-// 2e-37 below, where the exponential leaves the normal numbers; 0.5 z (1 + erf) has 1e-7 to 2e-7
-// for |z| < 1, and below loses all digits by z = -6 to the subtraction.  About 25 issue slots a value where erff takes over 60: the epilogue's
-// values are the exposed part of the first product (64,800 x 3072 x 768: 426 us with erff, 387
-// with this, 320 without any).  |z| is bounded in the tail only (z = +inf gives +inf; -inf and NaN
-// give NaN, as z Phi(z) does).
-__device__ __forceinline__ float gelu(float z) {
-  const float a = fminf(fabsf(z), 16.f);
-  const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3f, a, 1.f));
-  float q = 0.037535712f;
-  q = __builtin_fmaf(q, t, -0.16501968f);
-  q = __builtin_fmaf(q, t, 0.21997128f);
-  q = __builtin_fmaf(q, t, -0.06640263f);
-  q = __builtin_fmaf(q, t, 0.13542020f);
-  q = __builtin_fmaf(q, t, 0.097783938f);
-  q = __builtin_fmaf(q, t, 0.1211057f);
-  q = __builtin_fmaf(q, t, 0.11960549f);
-  const float e = __builtin_amdgcn_exp2f(a * a * -0.72134752f);  // exp(-a^2 / 2)
-  const float u = t * q * e;
-  return z > 0.f ? __builtin_fmaf(-a, u, z) : z * u;
-}
 
 // GEMM geometry of the register-staged kernel (column counts N that are not a multiple of
 // 256): workgroup tile 256 x BN (rows x columns of D), k-stage 64 (two MFMA k-steps per

@@ -1,0 +1,262 @@
+"""Python binding of the operators that train a network around the filter (include/afno.h): linear
+products with their epilogue, LayerNorm of a residual sum, dropout, each with its gradient.
+
+As in ``afno.py`` this is argument marshalling only.  Tensors are rows of channels with any leading
+shape ([B, H, W, C] grids, [M, C] tokens), float32 or bfloat16, contiguous, on one GPU.
+"""
+from __future__ import annotations
+
+import contextlib
+
+from .afno import (AFNO_ACT_GELU, AFNO_ACT_NONE, AFNO_ACT_RELU, _check, _dtype_code, _expect, _ptr,
+                   load_library)
+
+ACTIVATIONS = {"none": AFNO_ACT_NONE, "relu": AFNO_ACT_RELU, "gelu": AFNO_ACT_GELU}
+
+
+def afno_linear_forward(x, w, b, residual, M, K, N, activation, p, seed, offset, counter, dtype, out,
+                        pre, workspace, workspace_bytes, stream) -> int:
+    """Raw call: pointers as ints (or None), returns the C return code."""
+    return load_library().afno_linear_forward(x, w, b, residual, M, K, N, activation, p, seed, offset,
+                                              counter, dtype, out, pre, workspace, workspace_bytes,
+                                              stream)
+
+
+def afno_linear_backward(g, x, w, pre, M, K, N, activation, p, seed, offset, counter, dtype, dx, dw, db,
+                         workspace, workspace_bytes, stream) -> int:
+    return load_library().afno_linear_backward(g, x, w, pre, M, K, N, activation, p, seed, offset,
+                                               counter, dtype, dx, dw, db, workspace, workspace_bytes,
+                                               stream)
+
+
+def afno_layer_norm_forward(x, residual, gamma, beta, M, C, eps, dtype, out, sum_out, stream) -> int:
+    return load_library().afno_layer_norm_forward(x, residual, gamma, beta, M, C, eps, dtype, out,
+                                                  sum_out, stream)
+
+
+def afno_layer_norm_backward(g, x, gamma, gsum, M, C, eps, dtype, dx, dgamma, dbeta, workspace,
+                             workspace_bytes, stream) -> int:
+    return load_library().afno_layer_norm_backward(g, x, gamma, gsum, M, C, eps, dtype, dx, dgamma,
+                                                   dbeta, workspace, workspace_bytes, stream)
+
+
+def afno_dropout_forward(x, residual, n, p, seed, offset, counter, dtype, out, stream) -> int:
+    return load_library().afno_dropout_forward(x, residual, n, p, seed, offset, counter, dtype, out,
+                                               stream)
+
+
+def afno_dropout_backward(g, n, p, seed, offset, counter, dtype, dx, stream) -> int:
+    return load_library().afno_dropout_backward(g, n, p, seed, offset, counter, dtype, dx, stream)
+
+
+def afno_linear_forward_workspace(M, K, N, dtype) -> int:
+    """Bytes of workspace that the call may need, or a (negative) error code."""
+    return load_library().afno_linear_forward_workspace(M, K, N, dtype)
+
+
+def afno_linear_backward_workspace(M, K, N, dtype) -> int:
+    return load_library().afno_linear_backward_workspace(M, K, N, dtype)
+
+
+def afno_layer_norm_backward_workspace(M, C, dtype) -> int:
+    return load_library().afno_layer_norm_backward_workspace(M, C, dtype)
+
+
+# ---------------------------------------------------------------- torch-level wrappers
+
+
+def _rows(name, x, channels=None):
+    """(M, C) of a tensor seen as rows of channels."""
+    if x is None:
+        raise ValueError(f"{name} is missing")
+    if x.dim() < 1:
+        raise ValueError(f"{name} must have at least one dimension")
+    _dtype_code(x)
+    C = int(x.shape[-1])
+    if C == 0:
+        raise ValueError(f"{name} has no channels")
+    if channels is not None and C != channels:
+        raise ValueError(f"{name} has {C} channels, expected {channels}")
+    return x.numel() // C, C
+
+
+def _activation(activation) -> int:
+    if activation not in ACTIVATIONS:
+        raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}, got {activation!r}")
+    return ACTIVATIONS[activation]
+
+
+def _random(x, p, seed, offset, counter):
+    """Dropout's arguments checked: p, the two 64-bit numbers, the counter's address."""
+    for name, v in (("seed", seed), ("offset", offset)):
+        if not isinstance(v, int) or not 0 <= v < 2 ** 64:
+            raise ValueError(f"{name} must be an int in [0, 2^64), got {v!r}")
+    if counter is not None:
+        import torch
+        if counter.dtype != torch.int64 or counter.numel() != 1:
+            raise TypeError("counter must be an int64 tensor of one element")
+        if counter.device != x.device:
+            raise ValueError(f"counter is on {counter.device}, the input on {x.device}")
+    return float(p), seed, offset, None if counter is None else counter.data_ptr()
+
+
+@contextlib.contextmanager
+def _launching(x, stream, tensors):
+    """The call's stream handle, with x's device current and new tensors allocated for that stream.
+    A caller's stream other than torch's current one is recorded on the tensors it reads, so that
+    their memory is not handed out again before it has run."""
+    import torch
+    device = x.device
+    with contextlib.ExitStack() as stack:
+        if device.index != torch.cuda.current_device():
+            stack.enter_context(torch.cuda.device(device))
+        if stream is None:
+            yield torch._C._cuda_getCurrentRawStream(device.index)
+            return
+        if stream.device != device:
+            raise ValueError(f"stream is on {stream.device}, the tensors on {device}")
+        if stream.cuda_stream != torch._C._cuda_getCurrentRawStream(device.index):
+            stack.enter_context(torch.cuda.stream(stream))
+            for t in tensors:
+                if t is not None:
+                    t.record_stream(stream)
+        yield stream.cuda_stream
+
+
+def _workspace(x, nbytes: int):
+    """(address, bytes) of a workspace from torch's allocator, which a captured graph keeps, and the
+    tensor that holds it."""
+    import torch
+    _check(min(nbytes, 0))
+    if nbytes == 0:
+        return None, 0, None
+    t = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
+    return t.data_ptr(), nbytes, t
+
+
+def linear_forward(x, w, b=None, *, activation="none", residual=None, p=0.0, seed=0, offset=0,
+                   counter=None, out=None, pre=None, stream=None):
+    """out = drop(act(x w + b)) + residual for x [..., K], w [K, N], b [N] or None, residual and out
+    [..., N]; activation "none", "relu" or "gelu" (the exact one).  pre: a tensor like out that
+    receives x w + b, which linear_backward takes where there is an activation.
+
+    Dropout with probability p (in units of 2^-16; 0: none) keeps an element by its flat index, seed
+    and offset (+ counter[0], an int64 tensor on x's device that is read when the kernel runs): the
+    same numbers give the same mask, so a model gives each of its dropouts an offset range of its own
+    and counts its steps in counter.  Enqueued on ``stream`` (default: torch's current stream)."""
+    import torch
+    M, K = _rows("x", x)
+    if w is None or w.dim() != 2:
+        raise ValueError("w must be [K, N]")
+    N = int(w.shape[1])
+    shape = (*x.shape[:-1], N)
+    specs = [("w", w, (K, N), None)]
+    specs += [(n, t, s, None) for n, t, s in (("b", b, (N,)), ("residual", residual, shape),
+                                              ("out", out, shape), ("pre", pre, shape)) if t is not None]
+    _expect(x, specs)
+    act, drop = _activation(activation), _random(x, p, seed, offset, counter)
+    with _launching(x, stream, (x, w, b, residual, out, pre, counter)) as handle:
+        if out is None:
+            out = torch.empty(shape, dtype=x.dtype, device=x.device)
+        code = _dtype_code(x)
+        ws, nbytes, _held = _workspace(x, afno_linear_forward_workspace(M, K, N, code))
+        _check(afno_linear_forward(_ptr(x), _ptr(w), _ptr(b), _ptr(residual), M, K, N, act, *drop, code,
+                                   _ptr(out), _ptr(pre), ws, nbytes, handle))
+    return out
+
+
+def linear_backward(g, x, w, *, pre=None, activation="none", p=0.0, seed=0, offset=0, counter=None,
+                    bias=True, need_dx=True, need_dw=True, stream=None):
+    """Gradients of linear_forward for g = dL/dout [..., N] (the residual's gradient is g itself):
+    a dict with dx like x, dw like w, db [N], in x's dtype, None where bias, need_dx or need_dw says
+    that it is not wanted.  activation, p, seed, offset and the counter's value as in the forward
+    call, pre the tensor that it filled (not read without an activation)."""
+    import torch
+    M, K = _rows("x", x)
+    if w is None or w.dim() != 2:
+        raise ValueError("w must be [K, N]")
+    N = int(w.shape[1])
+    act = _activation(activation)
+    shape = (*x.shape[:-1], N)
+    specs = [("w", w, (K, N), None), ("g", g, shape, None)]
+    if act:
+        specs.append(("pre", pre, shape, None))
+    _expect(x, specs)
+    if not (bias or need_dx or need_dw):
+        raise ValueError("no gradient is asked for")
+    drop = _random(x, p, seed, offset, counter)
+    with _launching(x, stream, (g, x, w, pre, counter)) as handle:
+        dx = torch.empty_like(x) if need_dx else None
+        dw = torch.empty_like(w) if need_dw else None
+        db = torch.empty(N, dtype=x.dtype, device=x.device) if bias else None
+        code = _dtype_code(x)
+        ws, nbytes, _held = _workspace(x, afno_linear_backward_workspace(M, K, N, code))
+        _check(afno_linear_backward(_ptr(g), _ptr(x), _ptr(w), _ptr(pre) if act else None, M, K, N, act,
+                                    *drop, code, _ptr(dx), _ptr(dw), _ptr(db), ws, nbytes, handle))
+    return {"dx": dx, "dw": dw, "db": db}
+
+
+def layer_norm_forward(x, gamma, beta, *, eps=1e-6, residual=None, out=None, sum_out=None, stream=None):
+    """LayerNorm over the last axis of v = x + residual (rounded to x's dtype; None: v = x):
+    (v - mean) / sqrt(var + eps) * gamma + beta with the biased variance.  sum_out: a tensor like x
+    that receives v, the residual stream and what layer_norm_backward takes."""
+    import torch
+    M, C = _rows("x", x)
+    specs = [("gamma", gamma, (C,), None), ("beta", beta, (C,), None)]
+    specs += [(n, t, tuple(x.shape), None) for n, t in (("residual", residual), ("out", out),
+                                                         ("sum_out", sum_out)) if t is not None]
+    _expect(x, specs)
+    with _launching(x, stream, (x, gamma, beta, residual, out, sum_out)) as handle:
+        if out is None:
+            out = torch.empty_like(x)
+        _check(afno_layer_norm_forward(_ptr(x), _ptr(residual), _ptr(gamma), _ptr(beta), M, C, eps,
+                                       _dtype_code(x), _ptr(out), _ptr(sum_out), handle))
+    return out
+
+
+def layer_norm_backward(g, x, gamma, *, eps=1e-6, gsum=None, stream=None):
+    """Gradients of the norm of x (the v that the forward call stored) for g = dL/dout: a dict with dx
+    (x's dtype; gsum, the gradient that reaches v along the residual stream, is added to it) and
+    dgamma, dbeta (float32)."""
+    import torch
+    M, C = _rows("x", x)
+    specs = [("gamma", gamma, (C,), None), ("g", g, tuple(x.shape), None)]
+    if gsum is not None:
+        specs.append(("gsum", gsum, tuple(x.shape), None))
+    _expect(x, specs)
+    with _launching(x, stream, (g, x, gamma, gsum)) as handle:
+        dx = torch.empty_like(x)
+        dgamma = torch.empty(C, dtype=torch.float32, device=x.device)
+        dbeta = torch.empty(C, dtype=torch.float32, device=x.device)
+        code = _dtype_code(x)
+        ws, nbytes, _held = _workspace(x, afno_layer_norm_backward_workspace(M, C, code))
+        _check(afno_layer_norm_backward(_ptr(g), _ptr(x), _ptr(gamma), _ptr(gsum), M, C, eps, code,
+                                        _ptr(dx), _ptr(dgamma), _ptr(dbeta), ws, nbytes, handle))
+    return {"dx": dx, "dgamma": dgamma, "dbeta": dbeta}
+
+
+def dropout_forward(x, p, seed, *, offset=0, counter=None, residual=None, out=None, stream=None):
+    """drop(x) + residual for a tensor of any shape; dropout's numbers as in linear_forward."""
+    import torch
+    specs = [(n, t, tuple(x.shape), None) for n, t in (("residual", residual), ("out", out)) if t is not None]
+    code = _dtype_code(x)
+    _expect(x, specs)
+    drop = _random(x, p, seed, offset, counter)
+    with _launching(x, stream, (x, residual, out, counter)) as handle:
+        if out is None:
+            out = torch.empty_like(x)
+        _check(afno_dropout_forward(_ptr(x), _ptr(residual), x.numel(), *drop, code, _ptr(out), handle))
+    return out
+
+
+def dropout_backward(g, p, seed, *, offset=0, counter=None, out=None, stream=None):
+    """drop(g), the gradient of dropout_forward's x for g = dL/dout (the residual's is g)."""
+    import torch
+    code = _dtype_code(g)
+    _expect(g, [] if out is None else [("out", out, tuple(g.shape), None)])
+    drop = _random(g, p, seed, offset, counter)
+    with _launching(g, stream, (g, out, counter)) as handle:
+        if out is None:
+            out = torch.empty_like(g)
+        _check(afno_dropout_backward(_ptr(g), g.numel(), *drop, code, _ptr(out), handle))
+    return out
