@@ -6,7 +6,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "kernels_linear.h"
+#include "kernels_linear_dma.h"
 #include "kernels_norm.h"
 #include "train_internal.h"
 
@@ -38,27 +38,45 @@ void fill_zero(void* p, size_t bytes, hipStream_t st) {
 
 // How a product is cut: tiles, and splits of k whose sums join_splits adds.
 struct Cut {
-  int tile;  // 128 or 64: gemm_reg's square tile
+  int tile;  // 256: gemm_tile256; 128 or 64: gemm_reg's square tile
   int splits;
   int64_t kper;
 };
 
-// A tile row or column costs its whole tile, so 128 x 128 where that many tiles (times the splits that
-// leave 256 k's to each) give every CU one, else 64 x 64.  Splits until there are two workgroups a
-// CU, each with at least 128 k's.
-Cut cut_product(int64_t M, int64_t N, int64_t K) {
+// wide: the operands are what gemm_tile256 takes (bf16, multiples of 8, 16-byte aligned).  It runs one
+// workgroup a CU, so it is for products that give most CUs a tile, split over k if need be with 512
+// k's at least to each.  Else a tile row or column costs its whole tile, so 128 x 128 where that many
+// tiles (times the splits that leave 256 k's to each) give every CU one, else 64 x 64; splits until there
+// are two workgroups a CU, each with at least 128 k's.
+Cut cut_product(int64_t M, int64_t N, int64_t K, bool wide) {
   Cut c;
+  int64_t s;
+  if (wide) {
+    const int64_t t = ceil_div(M, 256) * ceil_div(N, 256);
+    s = t >= 128 ? 1 : std::max<int64_t>(1, std::min<int64_t>(256 / t, K / 512));
+    if (t * s >= 128) {
+      c.tile = 256;
+      c.kper = ceil_div(ceil_div(K, s), 64) * 64;
+      c.splits = (int)ceil_div(K, c.kper);
+      return c;
+    }
+  }
   const int64_t t128 = ceil_div(M, 128) * ceil_div(N, 128), t64 = ceil_div(M, 64) * ceil_div(N, 64);
   c.tile = M > 64 && N > 64 && t128 * std::max<int64_t>(1, K / 256) >= 256 ? 128 : 64;
   const int64_t t = c.tile == 128 ? t128 : t64;
-  int64_t s = std::min<int64_t>(ceil_div(512, t), std::max<int64_t>(1, K / (c.tile == 128 ? 256 : 128)));
+  s = std::min<int64_t>(ceil_div(512, t), std::max<int64_t>(1, K / (c.tile == 128 ? 256 : 128)));
   if (t >= 256) s = 1;
   c.kper = std::max<int64_t>(32, ceil_div(ceil_div(K, s), 32) * 32);
   c.splits = (int)std::max<int64_t>(1, ceil_div(K, c.kper));
   return c;
 }
-size_t part_bytes(int64_t M, int64_t N, const Cut& c) {
+size_t part_of(int64_t M, int64_t N, const Cut& c) {
   return c.splits > 1 ? (size_t)c.splits * M * N * sizeof(float) : 0;
+}
+// whatever the addresses turn out to be
+size_t part_bytes(int64_t M, int64_t N, int64_t K, int dtype) {
+  const size_t any = part_of(M, N, cut_product(M, N, K, false));
+  return dtype == 0 ? any : std::max(any, part_of(M, N, cut_product(M, N, K, true)));
 }
 
 template <typename T, bool AR, bool BR, int BM, int BN, bool VEC>
@@ -73,12 +91,21 @@ void run_reg(const GemmArgs<T>& g, int splits, hipStream_t st) {
 // One product with its epilogue; part: room for part_bytes.
 template <typename T, bool AR, bool BR>
 hipError_t product(GemmArgs<T> g, float* part, hipStream_t st) {
-  const Cut c = cut_product(g.M, g.N, g.K);
   constexpr int UE = Unit<T>::UE;
   const bool vec = g.lda % UE == 0 && g.ldb % UE == 0 && at16(g.a) && at16(g.b);
+  // (row-major operands have lda = M and ldb = N, k-major ones K)
+  const bool wide = sizeof(T) == 2 && vec && g.N % 8 == 0 && at16(g.e.out) && at16(g.e.pre) &&
+                    at16(g.e.residual);
+  const Cut c = cut_product(g.M, g.N, g.K, wide);
   g.kper = c.kper;
   g.part = c.splits > 1 ? part : nullptr;
-  by_flag(vec, [&](auto v) {
+  if (c.tile == 256) {
+    if constexpr (sizeof(T) == 2) {
+      const int64_t tiles = ceil_div(g.M, 256) * ceil_div(g.N, 256);
+      hipLaunchKernelGGL((gemm_tile256<AR, BR>), dim3((unsigned)(8 * ceil_div(tiles, 8)), (unsigned)c.splits),
+                         dim3(512), 0, st, g);
+    }
+  } else by_flag(vec, [&](auto v) {
     constexpr bool V = decltype(v)::value;
     if (c.tile == 128)
       run_reg<T, AR, BR, 128, 128, V>(g, c.splits, st);
@@ -113,8 +140,8 @@ BwdLayout layout(const LinearBwd& a) {
   if (a.db) at += up256((size_t)ceil_div(a.M, chunk_rows(a.M, a.N)) * a.N * sizeof(float));
   l.part = at;
   size_t p = 0;
-  if (a.dx) p = part_bytes(a.M, a.K, cut_product(a.M, a.K, a.N));
-  if (a.dw) p = std::max(p, part_bytes(a.K, a.N, cut_product(a.K, a.N, a.M)));
+  if (a.dx) p = part_bytes(a.M, a.K, a.N, a.dtype);
+  if (a.dw) p = std::max(p, part_bytes(a.K, a.N, a.M, a.dtype));
   l.bytes = at + p;
   return l;
 }
@@ -138,7 +165,7 @@ hipError_t set_train_attributes() {
 }
 
 size_t linear_forward_bytes(const LinearFwd& a) {
-  return part_bytes(a.M, a.N, cut_product(a.M, a.N, a.K));
+  return part_bytes(a.M, a.N, a.K, a.dtype);
 }
 
 hipError_t launch_linear_forward(const LinearFwd& a, void* ws, hipStream_t st) {

@@ -11,6 +11,7 @@
 
 namespace afno {
 
+typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 enum { kActNone = 0, kActRelu = 1, kActGelu = 2 };
 
 // what happens to a product's element (m, n) on its way out
@@ -66,6 +67,39 @@ __device__ __forceinline__ void finish(const Epilogue<T>& e, const Drop& d, int6
     if (e.residual) z += ld_f(e.residual + at);
     e.out[at] = Store<T>::to(z);
   }
+}
+
+// The same of eight neighbouring elements of bf16 from `at` on, a multiple of 8, with their biases; out,
+// pre and residual 16-byte aligned.  Streamed once: non-temporal, so that they do not push the
+// products' operands out of the caches.
+__device__ __forceinline__ void finish8(const Epilogue<bf16>& e, const Drop& d, int64_t at,
+                                        const float (&bias)[8], float (&o)[8]) {
+  auto store = [&](bf16* p) {
+    const u32x4 w = {cvt_pk(o[0], o[1]), cvt_pk(o[2], o[3]), cvt_pk(o[4], o[5]), cvt_pk(o[6], o[7])};
+    __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(p + at));
+  };
+#pragma unroll
+  for (int i = 0; i < 8; ++i) o[i] += bias[i];
+  if (e.pre) store(e.pre);
+  if (e.act == kActGelu) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = gelu(o[i]);
+  } else if (e.act == kActRelu) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = activate(o[i], kActRelu);
+  }
+  if (d.threshold) {
+    const uint4 w = d.numbers((uint64_t)at >> 3);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = d.apply(o[i], w, i);
+  }
+  if (e.residual) {
+    const u32x4 r = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(e.residual + at));
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      o[i] += i % 2 ? __uint_as_float(r[i / 2] & 0xffff0000u) : __uint_as_float(r[i / 2] << 16);
+  }
+  store(e.out);
 }
 
 // workgroup -> (tile row, tile column): workgroup g runs on XCD g % 8, and the workgroups of one XCD
@@ -281,11 +315,21 @@ __global__ void __launch_bounds__(256) join_splits(const float* __restrict__ par
   if (t >= M * per) return;
   const int64_t m = t / per, n = 4 * (t - m * per);
   float v[4] = {0.f, 0.f, 0.f, 0.f};
-  for (int s = 0; s < splits; ++s) {
-    const float* p = part + (s * M + m) * N + n;
+  const float* p = part + m * N + n;
+  if (N % 4 == 0) {  // 16-byte aligned: the workspace is
+    for (int s = 0; s < splits; ++s, p += M * N) {
+      const float4 w = *reinterpret_cast<const float4*>(p);
+      v[0] += w.x;
+      v[1] += w.y;
+      v[2] += w.z;
+      v[3] += w.w;
+    }
+  } else {
+    for (int s = 0; s < splits; ++s, p += M * N) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j)
-      if (n + j < N) v[j] += p[j];
+      for (int j = 0; j < 4; ++j)
+        if (n + j < N) v[j] += p[j];
+    }
   }
   const Drop d(e.drop);
   finish<T, 4>(e, d, N, m, n, N, v);

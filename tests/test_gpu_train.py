@@ -132,6 +132,9 @@ LINEAR = [
     (1000, 96, 384, "gelu", 0.0, True, False),
     (2049, 512, 256, "none", 0.1, True, True),
     (5000, 256, 640, "gelu", 0.1, True, False),
+    (8008, 200, 1032, "gelu", 0.1, True, True),       # many ragged tiles of 256, k behind the last whole stage
+    (4104, 2056, 264, "relu", 0.25, True, False),     # few of them, split over k
+    (8200, 40, 1024, "none", 0.0, False, True),       # less than one stage of k
 ]
 
 
