@@ -241,7 +241,8 @@ int afno_filter_backward(const void* x, const void* w1, const void* b1, const vo
  * the same bits.
  *
  * Workspace.  afno_*_workspace gives the bytes that a call of these sizes may need (0: none; an error
- * code for sizes that the call refuses).  With workspace non-NULL the call uses the caller's memory:
+ * code for sizes that the call refuses); aligned non-zero: for arrays that are all 16-byte aligned,
+ * which may need less (rows at other addresses are copied).  With workspace non-NULL the call uses the caller's memory:
  * at least that many bytes, 16-byte aligned, apart from every array, the call's alone until its work
  * has ended, so that captured graphs that may run at the same time need one each.  With NULL the
  * library takes one of its own as afno_filter_forward does, except under stream capture, where a
@@ -269,7 +270,7 @@ int afno_linear_forward(const void* x, const void* w, const void* b, const void*
                         int64_t K, int64_t N, int activation, float p, uint64_t seed,
                         uint64_t offset, const uint64_t* counter, int dtype, void* out, void* pre,
                         void* workspace, int64_t workspace_bytes, hipStream_t stream);
-int64_t afno_linear_forward_workspace(int64_t M, int64_t K, int64_t N, int dtype);
+int64_t afno_linear_forward_workspace(int64_t M, int64_t K, int64_t N, int dtype, int aligned);
 
 /*
  * afno_linear_backward -- gradients of afno_linear_forward for g = dL/dout (the residual's is g):
@@ -282,7 +283,7 @@ int afno_linear_backward(const void* g, const void* x, const void* w, const void
                          int64_t K, int64_t N, int activation, float p, uint64_t seed,
                          uint64_t offset, const uint64_t* counter, int dtype, void* dx, void* dw,
                          void* db, void* workspace, int64_t workspace_bytes, hipStream_t stream);
-int64_t afno_linear_backward_workspace(int64_t M, int64_t K, int64_t N, int dtype);
+int64_t afno_linear_backward_workspace(int64_t M, int64_t K, int64_t N, int dtype, int aligned);
 
 /*
  * afno_layer_norm_forward -- v = x + residual rounded to dtype (residual NULL: v = x);

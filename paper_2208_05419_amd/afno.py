@@ -104,8 +104,8 @@ def load_library():
     for name in ("linear_forward", "linear_backward", "layer_norm_forward", "layer_norm_backward",
                  "dropout_forward", "dropout_backward"):
         getattr(lib, "afno_" + name).restype = ci
-    lib.afno_linear_forward_workspace.argtypes = [i64, i64, i64, ci]
-    lib.afno_linear_backward_workspace.argtypes = [i64, i64, i64, ci]
+    lib.afno_linear_forward_workspace.argtypes = [i64, i64, i64, ci, ci]
+    lib.afno_linear_backward_workspace.argtypes = [i64, i64, i64, ci, ci]
     lib.afno_layer_norm_backward_workspace.argtypes = [i64, i64, ci]
     for name in ("linear_forward", "linear_backward", "layer_norm_backward"):
         getattr(lib, f"afno_{name}_workspace").restype = i64
@@ -256,18 +256,19 @@ def _expect(x, specs):
     shape, that dtype (None: x's), x's device and a contiguous layout, and that x is on the
     GPU: the C library trusts the sizes it is given, so a mismatched tensor would be read or
     written beyond its end."""
+    own, device = x.dtype, x.device
     for name, t, shape, dt in specs:
         if t is None:
             raise ValueError(f"{name} is missing")
-        if tuple(t.shape) != tuple(shape):
+        if t.shape != shape:  # a torch.Size compares as the tuple that it is
             raise ValueError(f"{name} has shape {tuple(t.shape)}, expected {tuple(shape)} "
                              "(weight shapes must match num_blocks, the block size and the "
                              "hidden size)")
-        want = x.dtype if dt is None else dt
+        want = own if dt is None else dt
         if t.dtype != want:
             raise TypeError(f"{name} has dtype {t.dtype}, expected {want}")
-        if t.device != x.device:
-            raise ValueError(f"{name} is on {t.device}, x on {x.device}")
+        if t.device != device:
+            raise ValueError(f"{name} is on {t.device}, x on {device}")
         if not t.is_contiguous():
             raise ValueError(f"{name} must be contiguous")
     if not x.is_contiguous():

@@ -234,6 +234,9 @@ int run_dropout(const void* x, const void* residual, int64_t n, float p, uint64_
 
 #undef AFNO_TRY
 
+// an address for the queries, with every gradient asked for: all that a call of some sizes may need
+const void* some_address(int aligned) { return reinterpret_cast<const void*>((uintptr_t)(aligned ? 16 : 4)); }
+
 template <typename F>
 int64_t workspace_of(int64_t M, int64_t K, int64_t N, int dtype, F bytes) {
   g_last_error.clear();
@@ -314,18 +317,18 @@ int afno_dropout_backward(const void* g, int64_t n, float p, uint64_t seed, uint
   });
 }
 
-int64_t afno_linear_forward_workspace(int64_t M, int64_t K, int64_t N, int dtype) {
+int64_t afno_linear_forward_workspace(int64_t M, int64_t K, int64_t N, int dtype, int aligned) {
   return workspace_of(M, K, N, dtype, [&] {
-    return afno::linear_forward_bytes({nullptr, nullptr, nullptr, nullptr, M, K, N, 0, dtype, {}, nullptr, nullptr});
+    const void* p = some_address(aligned);
+    return afno::linear_forward_bytes({p, p, nullptr, nullptr, M, K, N, 0, dtype, {}, nullptr, nullptr});
   });
 }
 
-int64_t afno_linear_backward_workspace(int64_t M, int64_t K, int64_t N, int dtype) {
-  // all that a call may need: every gradient, an activation
-  void* some = &g_last_error;
+int64_t afno_linear_backward_workspace(int64_t M, int64_t K, int64_t N, int dtype, int aligned) {
   return workspace_of(M, K, N, dtype, [&] {
-    return afno::linear_backward_bytes(
-        {nullptr, nullptr, nullptr, nullptr, M, K, N, AFNO_ACT_GELU, dtype, {}, some, some, some});
+    const void* p = some_address(aligned);
+    void* out = const_cast<void*>(p);
+    return afno::linear_backward_bytes({p, p, p, p, M, K, N, AFNO_ACT_GELU, dtype, {}, out, out, out});
   });
 }
 

@@ -53,6 +53,17 @@ struct Drop {
     const uint32_t r = j & 1 ? u >> 16 : u & 0xffffu;
     return r >= threshold ? v * scale : 0.f;
   }
+  // NV <= 8 neighbouring values from flat index e on, whose numbers may lie in two groups
+  template <int NV>
+  __device__ __forceinline__ void apply_from(float (&v)[NV], uint64_t e) const {
+    const uint4 w0 = numbers(e >> 3), w1 = numbers((e >> 3) + 1);
+    const int first = (int)(e & 7);
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const int j = first + i;
+      v[i] = j < 8 ? apply(v[i], w0, j) : apply(v[i], w1, j - 8);
+    }
+  }
   __device__ __forceinline__ float apply_at(float v, uint64_t e) const {
     return apply(v, numbers(e >> 3), (int)(e & 7));
   }

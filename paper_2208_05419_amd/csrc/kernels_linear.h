@@ -30,6 +30,7 @@ struct GemmArgs {
   const T *a, *b;
   int64_t lda, ldb;   // elements from one row (k for row-major operands) to the next
   int64_t M, N, K;
+  int64_t ma, nb;     // rows of a and b that are there to be read: M and N, or rounded up to a unit
   int64_t kper;       // k of one split, a multiple of the k-stage; splits = gridDim.y
   float* part;        // [splits][M][N] sums (splits > 1), else null
   Epilogue<T> e;
@@ -69,37 +70,80 @@ __device__ __forceinline__ void finish(const Epilogue<T>& e, const Drop& d, int6
   }
 }
 
-// The same of eight neighbouring elements of bf16 from `at` on, a multiple of 8, with their biases; out,
-// pre and residual 16-byte aligned.  Streamed once: non-temporal, so that they do not push the
-// products' operands out of the caches.
-__device__ __forceinline__ void finish8(const Epilogue<bf16>& e, const Drop& d, int64_t at,
-                                        const float (&bias)[8], float (&o)[8]) {
-  auto store = [&](bf16* p) {
-    const u32x4 w = {cvt_pk(o[0], o[1]), cvt_pk(o[2], o[3]), cvt_pk(o[4], o[5]), cvt_pk(o[6], o[7])};
-    __builtin_nontemporal_store(w, reinterpret_cast<u32x4*>(p + at));
+// The same of NV = 4 or 8 neighbouring elements from `at` on, all there, with their biases.  ALIGNED: at a
+// multiple of NV and out, pre and residual aligned to NV elements; streamed once: non-temporal, so that
+// they do not push the products' operands out of the caches.  Else the same loads and stores at any address.
+template <typename T, int NV, bool ALIGNED>
+__device__ __forceinline__ void finish_unit(const Epilogue<T>& e, const Drop& d, int64_t at,
+                                            const float (&bias)[NV], float (&o)[NV]) {
+  typedef uint32_t Words __attribute__((ext_vector_type(NV * sizeof(T) / 4)));
+  constexpr int NW = NV * sizeof(T) / 4;
+  auto store = [&](T* p) {
+    Words w;
+#pragma unroll
+    for (int i = 0; i < NW; ++i) {
+      if constexpr (sizeof(T) == 2) w[i] = cvt_pk(o[2 * i], o[2 * i + 1]);
+      else w[i] = __float_as_uint(o[i]);
+    }
+    if constexpr (ALIGNED) __builtin_nontemporal_store(w, reinterpret_cast<Words*>(p + at));
+    else __builtin_memcpy(p + at, &w, sizeof(w));
   };
 #pragma unroll
-  for (int i = 0; i < 8; ++i) o[i] += bias[i];
+  for (int i = 0; i < NV; ++i) o[i] += bias[i];
   if (e.pre) store(e.pre);
   if (e.act == kActGelu) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = gelu(o[i]);
+    for (int i = 0; i < NV; ++i) o[i] = gelu(o[i]);
   } else if (e.act == kActRelu) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = activate(o[i], kActRelu);
+    for (int i = 0; i < NV; ++i) o[i] = activate(o[i], kActRelu);
   }
   if (d.threshold) {
-    const uint4 w = d.numbers((uint64_t)at >> 3);
+    if constexpr (ALIGNED) {
+      uint4 w = d.numbers((uint64_t)at >> 3);
+      if (NV == 4 && (at & 4)) w = make_uint4(w.z, w.w, w.z, w.w);
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = d.apply(o[i], w, i);
+      for (int i = 0; i < NV; ++i) o[i] = d.apply(o[i], w, i);
+    } else {
+      d.apply_from(o, (uint64_t)at);
+    }
   }
   if (e.residual) {
-    const u32x4 r = __builtin_nontemporal_load(reinterpret_cast<const u32x4*>(e.residual + at));
+    Words r;
+    if constexpr (ALIGNED) r = __builtin_nontemporal_load(reinterpret_cast<const Words*>(e.residual + at));
+    else __builtin_memcpy(&r, e.residual + at, sizeof(r));
 #pragma unroll
-    for (int i = 0; i < 8; ++i)
-      o[i] += i % 2 ? __uint_as_float(r[i / 2] & 0xffff0000u) : __uint_as_float(r[i / 2] << 16);
+    for (int i = 0; i < NV; ++i) {
+      if constexpr (sizeof(T) == 2)
+        o[i] += i % 2 ? __uint_as_float(r[i / 2] & 0xffff0000u) : __uint_as_float(r[i / 2] << 16);
+      else
+        o[i] += __uint_as_float(r[i]);
+    }
   }
   store(e.out);
+}
+// whether NV neighbouring elements can go through it aligned
+template <typename T, int NV>
+__host__ __device__ __forceinline__ bool aligned_units(const Epilogue<T>& e, int64_t N) {
+  const uintptr_t all = (uintptr_t)e.out | (uintptr_t)e.pre | (uintptr_t)e.residual;
+  return N % NV == 0 && all % (NV * sizeof(T)) == 0;
+}
+// up to NV neighbouring elements of row m from column n on; `units`: aligned_units
+template <typename T, int NV>
+__device__ __forceinline__ void finish_some(const Epilogue<T>& e, const Drop& d, int64_t N, int64_t m, int64_t n,
+                                            const float (&bias)[NV], float (&v)[NV], bool units) {
+  if (units) {
+    finish_unit<T, NV, true>(e, d, m * N + n, bias, v);
+  } else if (n + NV <= N) {
+    finish_unit<T, NV, false>(e, d, m * N + n, bias, v);
+  } else {
+    finish<T, NV>(e, d, N, m, n, N, v);  // takes the bias itself
+  }
+}
+template <typename T, int NV>
+__device__ __forceinline__ void load_bias(const Epilogue<T>& e, int64_t N, int64_t n, float (&b)[NV]) {
+#pragma unroll
+  for (int j = 0; j < NV; ++j) b[j] = e.bias && n + j < N ? ld_f(e.bias + n + j) : 0.f;
 }
 
 // workgroup -> (tile row, tile column): workgroup g runs on XCD g % 8, and the workgroups of one XCD
@@ -115,14 +159,17 @@ __device__ __forceinline__ bool tile_of(int64_t ntile, int nbn, int64_t* mb, int
 // One 16-byte unit (UE elements along the operand's fastest index) in registers.
 template <typename T> struct Unit {
   static constexpr int UE = 16 / sizeof(T);
-  // elements p[0 .. n), the rest 0; n <= 0: none.  VEC: p is 16-byte aligned and n is never between
+  // elements p[0 .. n), the rest 0; n <= 0: none.  VEC: p is 16-byte aligned and n is never between.
+  // Else one load too where all are there: global memory takes it at any address.
   template <bool VEC>
   __device__ static uint4 load(const T* p, int64_t n) {
     union { uint4 u; T e[UE]; } r;
     r.u = make_uint4(0, 0, 0, 0);
     if constexpr (VEC) {
       if (n > 0) r.u = *reinterpret_cast<const uint4*>(p);
-    } else {
+    } else if (n >= UE) {
+      __builtin_memcpy(&r.u, p, 16);
+    } else if (n > 0) {
 #pragma unroll
       for (int i = 0; i < UE; ++i)
         if (i < n) r.e[i] = p[i];
@@ -145,23 +192,22 @@ __device__ __forceinline__ uint2 lds_read_tr(const void* p) {
 
 // ---------------------------------------------------------------- any size, any alignment
 //
-// Register-staged product: 256 threads, workgroup tile BM x BN, 2 x 2 waves, k-stages of 32 through
-// two LDS stages, the next stage's loads in flight during the present one's matrix instructions.
-// k-major operands lie in the LDS as [row][32 + pad] and row-major ones as [32][rows + pad], as they
+// Register-staged product: 256 threads, workgroup tile BM x BN, 2 x 2 waves, k-stages of 64 bf16 or 32
+// fp32 through two LDS stages, the next stage's loads in flight during the present one's matrix instructions.
+// k-major operands lie in the LDS as [row][k + pad] and row-major ones as [k][rows + pad], as they
 // come: the fp32 instruction takes single values from either, the bf16 one its eight k's from a row or
 // through the transposing LDS read.  The products are taken transposed (D's rows are n), so that a
 // lane holds four neighbouring columns of one row.
-// VEC: lda, ldb multiples of a 16-byte unit and both bases 16-byte aligned.
 template <typename T, bool AR, bool BR, int BM, int BN>
 struct RegGeo {
-  static constexpr int BK = 32, UE = Unit<T>::UE, PAD = UE;
+  static constexpr int BK = 128 / sizeof(T), UE = Unit<T>::UE, PAD = UE;
   static constexpr int LA = AR ? BM + PAD : BK + PAD, LB = BR ? BN + PAD : BK + PAD;  // LDS strides
   static constexpr int SA = (AR ? BK : BM) * LA, SB = (BR ? BK : BN) * LB;            // one stage
   static constexpr int UA = BM * BK / UE / 256, UB = BN * BK / UE / 256;              // units a thread
   static constexpr int kBytes = 2 * (SA + SB) * (int)sizeof(T);
 };
 
-template <typename T, bool AR, bool BR, int BM, int BN, bool VEC>
+template <typename T, bool AR, bool BR, int BM, int BN>
 __global__ void __launch_bounds__(256) gemm_reg(GemmArgs<T> g) {
   typedef RegGeo<T, AR, BR, BM, BN> G;
   constexpr int BK = G::BK, UE = G::UE, TM = BM / 32, TN = BN / 32;
@@ -183,12 +229,12 @@ __global__ void __launch_bounds__(256) gemm_reg(GemmArgs<T> g) {
     if constexpr (R) {
       const int per = bm / UE, kk = u / per, r = UE * (u - kk * per);
       const int64_t k = kb + kk;
-      return Unit<T>::template load<VEC>(p + k * ld + r0 + r, k < k1 ? rows - r0 - r : 0);
+      return Unit<T>::template load<false>(p + k * ld + r0 + r, k < k1 ? rows - r0 - r : 0);
     } else {
       constexpr int per = BK / UE;
       const int r = u / per, kk = UE * (u - r * per);
       const int64_t k = kb + kk;
-      return Unit<T>::template load<VEC>(p + (r0 + r) * ld + k, r0 + r < rows ? k1 - k : 0);
+      return Unit<T>::template load<false>(p + (r0 + r) * ld + k, r0 + r < rows ? k1 - k : 0);
     }
   };
   auto slot = [&](auto row_major, int bm, int ldl, int u) {
@@ -287,6 +333,7 @@ __global__ void __launch_bounds__(256) gemm_reg(GemmArgs<T> g) {
   }
 
   const Drop d(g.e.drop);
+  const bool units = aligned_units<T, 4>(g.e, g.N);
 #pragma unroll
   for (int a = 0; a < TM; ++a) {
     const int64_t m = m0 + BM / 2 * wm + 16 * a + l16;
@@ -294,16 +341,89 @@ __global__ void __launch_bounds__(256) gemm_reg(GemmArgs<T> g) {
 #pragma unroll
     for (int b = 0; b < TN; ++b) {
       const int64_t n = n0 + BN / 2 * wn + 16 * b + 4 * gq;
+      if (n >= g.N) continue;
       float v[4] = {acc[a][b][0], acc[a][b][1], acc[a][b][2], acc[a][b][3]};
       if (g.part) {
         float* p = g.part + (blockIdx.y * g.M + m) * g.N + n;
+        if (g.N % 4 == 0) {
+          *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
+        } else {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-          if (n + j < g.N) p[j] = v[j];
+          for (int j = 0; j < 4; ++j)
+            if (n + j < g.N) p[j] = v[j];
+        }
       } else {
-        finish<T, 4>(g.e, d, g.N, m, n, g.N, v);
+        float bv[4];
+        load_bias(g.e, g.N, n, bv);
+        finish_some(g.e, d, g.N, m, n, bv, v, units);
       }
     }
+  }
+}
+
+// ---------------------------------------------------------------- few rows
+//
+// D = x w of a few rows (serving: single tokens), where the weights' bytes are all the time there is:
+// each is read once per MR rows, on the vector ALUs, straight from memory.  A workgroup takes 32
+// columns and MR rows (blockIdx.y); its 16 waves take k's in turn, a load of a wave 32 columns of 16
+// (fp32 8) k's.  Each lane sums its columns, the 16 lanes of a DPP row add theirs in registers, and the
+// 64 DPP rows' sums meet in the LDS, added in order.  w row-major, at any address and of any width.
+template <int CTRL>
+__device__ __forceinline__ float dpp_add(float v) {
+  return v + __int_as_float(__builtin_amdgcn_update_dpp(0, __float_as_int(v), CTRL, 0xf, 0xf, true));
+}
+constexpr int kRowsCols = 32;  // 64 bytes of a row of bf16 weights: 16 columns, 1,024 of 4,096 k's: 9.7 us, 32: 6.6
+template <typename T, int MR>
+__global__ void __launch_bounds__(1024) linear_rows(GemmArgs<T> g) {
+  constexpr int UE = Unit<T>::UE, COLS = kRowsCols, LC = COLS / UE, KR = 64 / LC, PF = 4;
+  __shared__ float sums[64][MR * COLS];
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  const int64_t n = (int64_t)blockIdx.x * COLS + UE * (lane % LC), m0 = (int64_t)blockIdx.y * MR;
+  float acc[MR][UE];
+#pragma unroll
+  for (int r = 0; r < MR; ++r)
+#pragma unroll
+    for (int e = 0; e < UE; ++e) acc[r][e] = 0.f;
+  const T* w = g.b + n;
+  const int64_t here = g.N - n;  // columns of this lane's that are there
+  const T* x[MR];
+#pragma unroll
+  for (int r = 0; r < MR; ++r) x[r] = g.a + min(m0 + r, g.M - 1) * g.lda;
+  // PF loads of the weights under way in each lane
+  for (int64_t k0 = wave * KR + lane / LC; k0 < g.K; k0 += 16 * KR * PF) {
+    union { uint4 u; T e[UE]; } wv[PF];
+    float xv[PF][MR];
+#pragma unroll
+    for (int i = 0; i < PF; ++i) {
+      const int64_t k = k0 + 16 * KR * i;
+      wv[i].u = Unit<T>::template load<false>(w + k * g.ldb, k < g.K ? here : 0);
+#pragma unroll
+      for (int r = 0; r < MR; ++r) xv[i][r] = k < g.K ? ld_f(x[r] + k) : 0.f;
+    }
+#pragma unroll
+    for (int i = 0; i < PF; ++i)
+#pragma unroll
+      for (int r = 0; r < MR; ++r)
+#pragma unroll
+        for (int e = 0; e < UE; ++e) acc[r][e] = __builtin_fmaf(xv[i][r], (float)wv[i].e[e], acc[r][e]);
+  }
+#pragma unroll
+  for (int r = 0; r < MR; ++r)
+#pragma unroll
+    for (int e = 0; e < UE; ++e) {
+      float v = acc[r][e];
+      v = dpp_add<0x128>(v);                      // row_ror:8
+      if constexpr (LC <= 4) v = dpp_add<0x124>(v);  // row_ror:4
+      if ((lane & 15) < LC) sums[tid >> 4][r * COLS + UE * (lane & 15) + e] = v;
+    }
+  __syncthreads();
+  const Drop d(g.e.drop);
+  for (int i = tid; i < MR * COLS; i += 1024) {
+    const int64_t m = m0 + i / COLS, c = (int64_t)blockIdx.x * COLS + i % COLS;
+    if (m >= g.M || c >= g.N) continue;
+    float v[1] = {0.f};
+    for (int j = 0; j < 64; ++j) v[0] += sums[j][i];
+    finish<T, 1>(g.e, d, g.N, m, c, g.N, v);
   }
 }
 
@@ -332,101 +452,128 @@ __global__ void __launch_bounds__(256) join_splits(const float* __restrict__ par
     }
   }
   const Drop d(e.drop);
-  finish<T, 4>(e, d, N, m, n, N, v);
+  float bv[4];
+  load_bias(e, N, n, bv);
+  finish_some(e, d, N, m, n, bv, v, aligned_units<T, 4>(e, N));
 }
 
 // ---------------------------------------------------------------- dz and the bias gradient
 //
 // dz = act'(pre) drop(g), rounded to T for the matrix cores (the one rounding of the backward pass
-// before its results'), and the sums over chunks of rows of the unrounded dz, part [chunks][N].  A
-// workgroup takes the rows of one chunk (blockIdx.y) and 256 columns: VEC (N a multiple of 8, all
-// bases 16-byte aligned) 32 threads of eight columns by eight rows at a time, whose sums meet in the
-// LDS; else a column a thread.  dz or part may be null.
+// before its results'), rows of ldz values, zeros behind the N of dz; and the sums over chunks of rows of the
+// unrounded dz, part [chunks][N].  A workgroup takes the rows of one chunk (blockIdx.y) and 256 columns:
+// 32 threads of eight columns by eight rows at a time, whose sums meet in the LDS.  VEC: N a multiple of 8,
+// g and pre 16-byte aligned.  dz (16-byte aligned, ldz a multiple of 8) or part may be null.
 template <typename T, bool VEC>
 __global__ void __launch_bounds__(256) dz_kernel(const T* __restrict__ g, const T* __restrict__ pre,
-                                                 T* __restrict__ dz, float* __restrict__ part,
-                                                 int64_t M, int64_t N, int64_t rows, int act,
-                                                 DropArgs da) {
+                                                 T* __restrict__ dz, int64_t ldz, float* __restrict__ part,
+                                                 int64_t M, int64_t N, int64_t rows, int act, DropArgs da) {
+  __shared__ float sums[8][256];
+  constexpr int UE = Unit<T>::UE, NU = 8 / UE;
   const int64_t m0 = blockIdx.y * rows, m1 = min(M, m0 + rows);
   const Drop d(da);
-  if constexpr (!VEC) {
-    const int64_t n = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (n >= N) return;
-    float s = 0.f;
-    for (int64_t m = m0; m < m1; ++m) {
+  const int c = 8 * (threadIdx.x & 31), r = threadIdx.x >> 5;
+  const int64_t n = (int64_t)blockIdx.x * 256 + c;
+  float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if (n < N) {
+    for (int64_t m = m0 + r; m < m1; m += 8) {
       const int64_t at = m * N + n;
-      float v = ld_f(g + at);
-      if (d.threshold) v = d.apply_at(v, (uint64_t)at);
-      if (act) v *= activation_slope(ld_f(pre + at), act);
-      if (dz) dz[at] = Store<T>::to(v);
-      s += v;
-    }
-    if (part) part[blockIdx.y * N + n] = s;
-  } else {
-    __shared__ float sums[8][256];
-    constexpr int UE = Unit<T>::UE, NU = 8 / UE;
-    const int c = 8 * (threadIdx.x & 31), r = threadIdx.x >> 5;
-    const int64_t n = (int64_t)blockIdx.x * 256 + c;
-    float s[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
-    if (n < N) {
-      for (int64_t m = m0 + r; m < m1; m += 8) {
-        const int64_t at = m * N + n;
-        union { uint4 u[NU]; T e[8]; } gv, pv, ov;
+      union { uint4 u[NU]; T e[8]; } gv, pv, ov;
 #pragma unroll
-        for (int i = 0; i < NU; ++i) gv.u[i] = reinterpret_cast<const uint4*>(g + at)[i];
-        if (act) {
+      for (int i = 0; i < NU; ++i) gv.u[i] = Unit<T>::template load<VEC>(g + at + UE * i, N - n - UE * i);
+      if (act) {
 #pragma unroll
-          for (int i = 0; i < NU; ++i) pv.u[i] = reinterpret_cast<const uint4*>(pre + at)[i];
-        }
-        uint4 w = make_uint4(0, 0, 0, 0);
-        if (d.threshold) w = d.numbers((uint64_t)at >> 3);
+        for (int i = 0; i < NU; ++i) pv.u[i] = Unit<T>::template load<VEC>(pre + at + UE * i, N - n - UE * i);
+      }
+      float v[8];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-          float v = (float)gv.e[j];
-          if (d.threshold) v = d.apply(v, w, j);
-          if (act) v *= activation_slope((float)pv.e[j], act);
-          s[j] += v;
-          ov.e[j] = Store<T>::to(v);
-        }
-        if (dz) {
+      for (int j = 0; j < 8; ++j) v[j] = (float)gv.e[j];
+      if (d.threshold) {
+        if constexpr (VEC) {
+          const uint4 w = d.numbers((uint64_t)at >> 3);
 #pragma unroll
-          for (int i = 0; i < NU; ++i) reinterpret_cast<uint4*>(dz + at)[i] = ov.u[i];
+          for (int j = 0; j < 8; ++j) v[j] = d.apply(v[j], w, j);
+        } else {
+          d.apply_from(v, (uint64_t)at);
         }
       }
-    }
-    if (!part) return;
 #pragma unroll
-    for (int j = 0; j < 8; ++j) sums[r][c + j] = s[j];
-    __syncthreads();
-    const int64_t col = (int64_t)blockIdx.x * 256 + threadIdx.x;
-    if (col < N) {
-      float t = 0.f;
+      for (int j = 0; j < 8; ++j) {
+        if (act) v[j] *= activation_slope((float)pv.e[j], act);
+        if (!VEC && n + j >= N) v[j] = 0.f;
+        s[j] += v[j];
+        ov.e[j] = Store<T>::to(v[j]);
+      }
+      if (dz) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) t += sums[i][threadIdx.x];
-      part[blockIdx.y * N + col] = t;
+        for (int i = 0; i < NU; ++i) reinterpret_cast<uint4*>(dz + m * ldz + n)[i] = ov.u[i];
+      }
     }
+  }
+  if (!part) return;
+#pragma unroll
+  for (int j = 0; j < 8; ++j) sums[r][c + j] = s[j];
+  __syncthreads();
+  const int64_t col = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  if (col < N) {
+    float t = 0.f;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) t += sums[i][threadIdx.x];
+    part[blockIdx.y * N + col] = t;
   }
 }
 
-// The sums over `chunks` of part[chunk][n], n < N, in an order that does not change: 16 threads of a
-// column take every sixteenth chunk, then their sums are added.  16 columns a workgroup.  Columns from
-// `first` on go to out2.
+// Rows of `cols` values at any address copied to rows of ld (a multiple of a 16-byte unit), zeros behind
+// them, so that the direct-to-LDS kernels can take them: two arrays in one launch, the units of the first,
+// then the second's (rows2 = 0: none).
 template <typename T>
-__global__ void __launch_bounds__(256) join_columns(const float* __restrict__ part, int chunks,
-                                                    int64_t N, int64_t first, T* __restrict__ out,
-                                                    T* __restrict__ out2) {
-  __shared__ float sums[16][17];
+struct PackArgs {
+  const T* src;
+  T* dst;
+  int64_t rows, cols, ld;
+};
+template <typename T>
+__global__ void __launch_bounds__(256) pack_rows(PackArgs<T> a, PackArgs<T> b) {
+  constexpr int UE = Unit<T>::UE;
+  int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t na = a.rows * (a.ld / UE);
+  const bool second = u >= na;
+  if (second) u -= na;
+  const PackArgs<T> p = second ? b : a;
+  if (!p.rows) return;
+  const int64_t per = p.ld / UE, r = u / per, c = UE * (u - r * per);
+  if (r >= p.rows) return;
+  const uint4 w = Unit<T>::template load<false>(p.src + r * p.cols + c, p.cols - c);
+  *reinterpret_cast<uint4*>(p.dst + r * p.ld + c) = w;
+}
+
+// The sums over `chunks` of part[chunk][n], n < N, in an order that does not change: 64 threads of a
+// column take every 64th chunk, then their sums are added.  16 columns a workgroup.  Columns from `first` on
+// go to out2.  Eight chunks' loads are under way at a time: one after another they took longer than the
+// kernel that made them (512 chunks of 666 columns: 17 of 29 us).
+template <typename T>
+__global__ void __launch_bounds__(1024) join_columns(const float* __restrict__ part, int chunks,
+                                                     int64_t N, int64_t first, T* __restrict__ out,
+                                                     T* __restrict__ out2) {
+  __shared__ float sums[64][17];
   const int c = threadIdx.x & 15, r = threadIdx.x >> 4;
   const int64_t n = (int64_t)blockIdx.x * 16 + c;
   float s = 0.f;
-  if (n < N)
-    for (int i = r; i < chunks; i += 16) s += part[(int64_t)i * N + n];
+  if (n < N) {
+    for (int i = r; i < chunks; i += 512) {
+      float v[8];
+#pragma unroll
+      for (int j = 0; j < 8; ++j) v[j] = i + 64 * j < chunks ? part[(int64_t)(i + 64 * j) * N + n] : 0.f;
+#pragma unroll
+      for (int j = 0; j < 8; ++j) s += v[j];
+    }
+  }
   sums[r][c] = s;
   __syncthreads();
   if (r == 0 && n < N) {
     float t = 0.f;
 #pragma unroll
-    for (int i = 0; i < 16; ++i) t += sums[i][c];
+    for (int i = 0; i < 64; ++i) t += sums[i][c];
     if (n < first)
       out[n] = Store<T>::to(t);
     else

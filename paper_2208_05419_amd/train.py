@@ -7,8 +7,9 @@ shape ([B, H, W, C] grids, [M, C] tokens), float32 or bfloat16, contiguous, on o
 from __future__ import annotations
 
 import contextlib
+import functools
 
-from .afno import (AFNO_ACT_GELU, AFNO_ACT_NONE, AFNO_ACT_RELU, _check, _dtype_code, _expect, _ptr,
+from .afno import (AFNO_ACT_GELU, AFNO_ACT_NONE, AFNO_ACT_RELU, _check, _dtype_code, _expect,
                    load_library)
 
 ACTIVATIONS = {"none": AFNO_ACT_NONE, "relu": AFNO_ACT_RELU, "gelu": AFNO_ACT_GELU}
@@ -49,13 +50,13 @@ def afno_dropout_backward(g, n, p, seed, offset, counter, dtype, dx, stream) -> 
     return load_library().afno_dropout_backward(g, n, p, seed, offset, counter, dtype, dx, stream)
 
 
-def afno_linear_forward_workspace(M, K, N, dtype) -> int:
+def afno_linear_forward_workspace(M, K, N, dtype, aligned) -> int:
     """Bytes of workspace that the call may need, or a (negative) error code."""
-    return load_library().afno_linear_forward_workspace(M, K, N, dtype)
+    return load_library().afno_linear_forward_workspace(M, K, N, dtype, aligned)
 
 
-def afno_linear_backward_workspace(M, K, N, dtype) -> int:
-    return load_library().afno_linear_backward_workspace(M, K, N, dtype)
+def afno_linear_backward_workspace(M, K, N, dtype, aligned) -> int:
+    return load_library().afno_linear_backward_workspace(M, K, N, dtype, aligned)
 
 
 def afno_layer_norm_backward_workspace(M, C, dtype) -> int:
@@ -65,7 +66,17 @@ def afno_layer_norm_backward_workspace(M, C, dtype) -> int:
 # ---------------------------------------------------------------- torch-level wrappers
 
 
-def _rows(name, x, channels=None):
+def _address(t):
+    """Address of a tensor that _expect has checked, or None."""
+    return None if t is None else t.data_ptr() or None
+
+
+def _aligned(*addresses) -> bool:
+    """Whether all are multiples of 16 (None counts)."""
+    return all(not a or a % 16 == 0 for a in addresses)
+
+
+def _rows(name, x):
     """(M, C) of a tensor seen as rows of channels."""
     if x is None:
         raise ValueError(f"{name} is missing")
@@ -75,8 +86,6 @@ def _rows(name, x, channels=None):
     C = int(x.shape[-1])
     if C == 0:
         raise ValueError(f"{name} has no channels")
-    if channels is not None and C != channels:
-        raise ValueError(f"{name} has {C} channels, expected {channels}")
     return x.numel() // C, C
 
 
@@ -100,34 +109,42 @@ def _random(x, p, seed, offset, counter):
     return float(p), seed, offset, None if counter is None else counter.data_ptr()
 
 
-@contextlib.contextmanager
-def _launching(x, stream, tensors):
-    """The call's stream handle, with x's device current and new tensors allocated for that stream.
-    A caller's stream other than torch's current one is recorded on the tensors it reads, so that
-    their memory is not handed out again before it has run."""
+def _launch(x, stream, tensors, call):
+    """call(stream handle) with x's device current and new tensors allocated for that stream.  A
+    caller's stream other than torch's current one is recorded on the tensors that the call reads, so
+    that their memory is not handed out again before it has run."""
     import torch
-    device = x.device
+    device = x.get_device()
+    here = torch._C._cuda_getDevice() == device
+    if stream is None and here:
+        return call(torch._C._cuda_getCurrentRawStream(device))
     with contextlib.ExitStack() as stack:
-        if device.index != torch.cuda.current_device():
+        if not here:
             stack.enter_context(torch.cuda.device(device))
         if stream is None:
-            yield torch._C._cuda_getCurrentRawStream(device.index)
-            return
-        if stream.device != device:
-            raise ValueError(f"stream is on {stream.device}, the tensors on {device}")
-        if stream.cuda_stream != torch._C._cuda_getCurrentRawStream(device.index):
+            return call(torch._C._cuda_getCurrentRawStream(device))
+        if stream.device != x.device:
+            raise ValueError(f"stream is on {stream.device}, the tensors on {x.device}")
+        if stream.cuda_stream != torch._C._cuda_getCurrentRawStream(device):
             stack.enter_context(torch.cuda.stream(stream))
             for t in tensors:
                 if t is not None:
                     t.record_stream(stream)
-        yield stream.cuda_stream
+        return call(stream.cuda_stream)
+
+
+@functools.lru_cache(maxsize=1024)
+def _bytes(query, *sizes) -> int:
+    """The workspace query of these sizes (a function of them alone)."""
+    n = query(*sizes)
+    _check(min(n, 0))
+    return n
 
 
 def _workspace(x, nbytes: int):
     """(address, bytes) of a workspace from torch's allocator, which a captured graph keeps, and the
     tensor that holds it."""
     import torch
-    _check(min(nbytes, 0))
     if nbytes == 0:
         return None, 0, None
     t = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
@@ -155,14 +172,18 @@ def linear_forward(x, w, b=None, *, activation="none", residual=None, p=0.0, see
                                               ("out", out, shape), ("pre", pre, shape)) if t is not None]
     _expect(x, specs)
     act, drop = _activation(activation), _random(x, p, seed, offset, counter)
-    with _launching(x, stream, (x, w, b, residual, out, pre, counter)) as handle:
-        if out is None:
-            out = torch.empty(shape, dtype=x.dtype, device=x.device)
-        code = _dtype_code(x)
-        ws, nbytes, _held = _workspace(x, afno_linear_forward_workspace(M, K, N, code))
-        _check(afno_linear_forward(_ptr(x), _ptr(w), _ptr(b), _ptr(residual), M, K, N, act, *drop, code,
-                                   _ptr(out), _ptr(pre), ws, nbytes, handle))
-    return out
+    code = _dtype_code(x)
+
+    def call(handle):
+        y = torch.empty(shape, dtype=x.dtype, device=x.device) if out is None else out
+        px, pw = _address(x), _address(w)
+        ws, nbytes, _held = _workspace(x, _bytes(afno_linear_forward_workspace, M, K, N, code,
+                                                 _aligned(px, pw)))
+        _check(afno_linear_forward(px, pw, _address(b), _address(residual), M, K, N, act, *drop,
+                                   code, _address(y), _address(pre), ws, nbytes, handle))
+        return y
+
+    return _launch(x, stream, (x, w, b, residual, out, pre, counter), call)
 
 
 def linear_backward(g, x, w, *, pre=None, activation="none", p=0.0, seed=0, offset=0, counter=None,
@@ -185,15 +206,20 @@ def linear_backward(g, x, w, *, pre=None, activation="none", p=0.0, seed=0, offs
     if not (bias or need_dx or need_dw):
         raise ValueError("no gradient is asked for")
     drop = _random(x, p, seed, offset, counter)
-    with _launching(x, stream, (g, x, w, pre, counter)) as handle:
+    code = _dtype_code(x)
+
+    def call(handle):
         dx = torch.empty_like(x) if need_dx else None
         dw = torch.empty_like(w) if need_dw else None
         db = torch.empty(N, dtype=x.dtype, device=x.device) if bias else None
-        code = _dtype_code(x)
-        ws, nbytes, _held = _workspace(x, afno_linear_backward_workspace(M, K, N, code))
-        _check(afno_linear_backward(_ptr(g), _ptr(x), _ptr(w), _ptr(pre) if act else None, M, K, N, act,
-                                    *drop, code, _ptr(dx), _ptr(dw), _ptr(db), ws, nbytes, handle))
-    return {"dx": dx, "dw": dw, "db": db}
+        pg, px, pw = _address(g), _address(x), _address(w)
+        ws, nbytes, _held = _workspace(x, _bytes(afno_linear_backward_workspace, M, K, N, code,
+                                                 _aligned(pg, px, pw)))
+        _check(afno_linear_backward(pg, px, pw, _address(pre) if act else None, M, K, N,
+                                    act, *drop, code, _address(dx), _address(dw), _address(db), ws, nbytes, handle))
+        return {"dx": dx, "dw": dw, "db": db}
+
+    return _launch(x, stream, (g, x, w, pre, counter), call)
 
 
 def layer_norm_forward(x, gamma, beta, *, eps=1e-6, residual=None, out=None, sum_out=None, stream=None):
@@ -206,12 +232,15 @@ def layer_norm_forward(x, gamma, beta, *, eps=1e-6, residual=None, out=None, sum
     specs += [(n, t, tuple(x.shape), None) for n, t in (("residual", residual), ("out", out),
                                                          ("sum_out", sum_out)) if t is not None]
     _expect(x, specs)
-    with _launching(x, stream, (x, gamma, beta, residual, out, sum_out)) as handle:
-        if out is None:
-            out = torch.empty_like(x)
-        _check(afno_layer_norm_forward(_ptr(x), _ptr(residual), _ptr(gamma), _ptr(beta), M, C, eps,
-                                       _dtype_code(x), _ptr(out), _ptr(sum_out), handle))
-    return out
+    code = _dtype_code(x)
+
+    def call(handle):
+        y = torch.empty_like(x) if out is None else out
+        _check(afno_layer_norm_forward(_address(x), _address(residual), _address(gamma), _address(beta), M, C, eps,
+                                       code, _address(y), _address(sum_out), handle))
+        return y
+
+    return _launch(x, stream, (x, gamma, beta, residual, out, sum_out), call)
 
 
 def layer_norm_backward(g, x, gamma, *, eps=1e-6, gsum=None, stream=None):
@@ -224,15 +253,18 @@ def layer_norm_backward(g, x, gamma, *, eps=1e-6, gsum=None, stream=None):
     if gsum is not None:
         specs.append(("gsum", gsum, tuple(x.shape), None))
     _expect(x, specs)
-    with _launching(x, stream, (g, x, gamma, gsum)) as handle:
+    code = _dtype_code(x)
+
+    def call(handle):
         dx = torch.empty_like(x)
         dgamma = torch.empty(C, dtype=torch.float32, device=x.device)
         dbeta = torch.empty(C, dtype=torch.float32, device=x.device)
-        code = _dtype_code(x)
-        ws, nbytes, _held = _workspace(x, afno_layer_norm_backward_workspace(M, C, code))
-        _check(afno_layer_norm_backward(_ptr(g), _ptr(x), _ptr(gamma), _ptr(gsum), M, C, eps, code,
-                                        _ptr(dx), _ptr(dgamma), _ptr(dbeta), ws, nbytes, handle))
-    return {"dx": dx, "dgamma": dgamma, "dbeta": dbeta}
+        ws, nbytes, _held = _workspace(x, _bytes(afno_layer_norm_backward_workspace, M, C, code))
+        _check(afno_layer_norm_backward(_address(g), _address(x), _address(gamma), _address(gsum), M, C, eps, code,
+                                        _address(dx), _address(dgamma), _address(dbeta), ws, nbytes, handle))
+        return {"dx": dx, "dgamma": dgamma, "dbeta": dbeta}
+
+    return _launch(x, stream, (g, x, gamma, gsum), call)
 
 
 def dropout_forward(x, p, seed, *, offset=0, counter=None, residual=None, out=None, stream=None):
@@ -242,11 +274,13 @@ def dropout_forward(x, p, seed, *, offset=0, counter=None, residual=None, out=No
     code = _dtype_code(x)
     _expect(x, specs)
     drop = _random(x, p, seed, offset, counter)
-    with _launching(x, stream, (x, residual, out, counter)) as handle:
-        if out is None:
-            out = torch.empty_like(x)
-        _check(afno_dropout_forward(_ptr(x), _ptr(residual), x.numel(), *drop, code, _ptr(out), handle))
-    return out
+
+    def call(handle):
+        y = torch.empty_like(x) if out is None else out
+        _check(afno_dropout_forward(_address(x), _address(residual), x.numel(), *drop, code, _address(y), handle))
+        return y
+
+    return _launch(x, stream, (x, residual, out, counter), call)
 
 
 def dropout_backward(g, p, seed, *, offset=0, counter=None, out=None, stream=None):
@@ -255,8 +289,10 @@ def dropout_backward(g, p, seed, *, offset=0, counter=None, out=None, stream=Non
     code = _dtype_code(g)
     _expect(g, [] if out is None else [("out", out, tuple(g.shape), None)])
     drop = _random(g, p, seed, offset, counter)
-    with _launching(g, stream, (g, out, counter)) as handle:
-        if out is None:
-            out = torch.empty_like(g)
-        _check(afno_dropout_backward(_ptr(g), g.numel(), *drop, code, _ptr(out), handle))
-    return out
+
+    def call(handle):
+        dx = torch.empty_like(g) if out is None else out
+        _check(afno_dropout_backward(_address(g), g.numel(), *drop, code, _address(dx), handle))
+        return dx
+
+    return _launch(g, stream, (g, out, counter), call)

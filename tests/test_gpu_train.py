@@ -135,6 +135,11 @@ LINEAR = [
     (8008, 200, 1032, "gelu", 0.1, True, True),       # many ragged tiles of 256, k behind the last whole stage
     (4104, 2056, 264, "relu", 0.25, True, False),     # few of them, split over k
     (8200, 40, 1024, "none", 0.0, False, True),       # less than one stage of k
+    (4111, 333, 205, "gelu", 0.1, True, True),        # rows that are no 16-byte units, copied to some that are
+    (2050, 1029, 516, "relu", 0.0, True, False),
+    (10, 513, 4099, "gelu", 0.1, True, False),        # few rows
+    (16, 1040, 520, "none", 0.0, True, True),
+    (16500, 264, 1544, "gelu", 0.3, False, False),    # over the tiles of all CUs
 ]
 
 
@@ -146,7 +151,8 @@ def test_linear(case, dtype):
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
-@pytest.mark.parametrize("case", [(5, 64, 128, "gelu", 0.2), (130, 256, 264, "relu", 0.0), (600, 128, 512, "gelu", 0.1)])
+@pytest.mark.parametrize("case", [(1, 64, 128, "gelu", 0.2), (130, 256, 264, "relu", 0.0), (600, 128, 512, "gelu", 0.1),
+                                  (5000, 136, 264, "gelu", 0.1)])
 def test_linear_at_odd_addresses(case, dtype):
     check_linear(*case[:3], dtype, case[3], case[4], residual=True, odd=True)
 
@@ -492,7 +498,7 @@ def test_workspaces_through_the_c_abi():
     r = np.random.default_rng(0)
     (_, x), (_, w), (_, g) = (store(r.standard_normal(s), "bf16") for s in ((M, K), (K, N), (M, N)))
     want = afno.linear_backward(g, x, w, p=0.1, seed=3)
-    need = afno.afno_linear_backward_workspace(M, K, N, afno.AFNO_DTYPE_BF16)
+    need = afno.afno_linear_backward_workspace(M, K, N, afno.AFNO_DTYPE_BF16, 1)
     outs = [torch.empty_like(t) for t in (want["dx"], want["dw"], want["db"])]
     st = torch.cuda.current_stream().cuda_stream
 

@@ -90,15 +90,20 @@ def test_nothing_to_do_needs_no_gpu():
 
 
 def test_workspace_sizes():
-    for f, sizes in ((afno.afno_linear_forward_workspace, (16, 64, 32)), (afno.afno_linear_backward_workspace, (16, 64, 32)),
-                     (afno.afno_layer_norm_backward_workspace, (16, 64))):
-        assert f(*sizes, 0) >= 0 and f(*sizes, BF16) >= 0
-        assert f(0, *sizes[1:], 0) == 0
-        assert f(-1, *sizes[1:], 0) == INV and f(sizes[0], 0, *sizes[2:], 0) == INV and f(*sizes, 5) == INV
-        assert f(2 ** 31, *sizes[1:], 0) == UNS
-    # the factor dz and the chunks' sums at least
-    assert afno.afno_linear_backward_workspace(1000, 64, 32, 0) >= 1000 * 32 * 4 + 32 * 4
+    for f, sizes, more in ((afno.afno_linear_forward_workspace, (16, 64, 32), (1,)),
+                           (afno.afno_linear_forward_workspace, (16, 64, 32), (0,)),
+                           (afno.afno_linear_backward_workspace, (16, 64, 32), (1,)),
+                           (afno.afno_layer_norm_backward_workspace, (16, 64), ())):
+        assert f(*sizes, 0, *more) >= 0 and f(*sizes, BF16, *more) >= 0
+        assert f(0, *sizes[1:], 0, *more) == 0
+        assert f(-1, *sizes[1:], 0, *more) == INV and f(sizes[0], 0, *sizes[2:], 0, *more) == INV
+        assert f(*sizes, 5, *more) == INV and f(2 ** 31, *sizes[1:], 0, *more) == UNS
+    # the factor dz and the chunks' sums at least, and copies of rows that are no 16-byte units
+    assert afno.afno_linear_backward_workspace(1000, 64, 32, 0, 1) >= 1000 * 32 * 4 + 32 * 4
     assert afno.afno_layer_norm_backward_workspace(1000, 64, 0) >= 2 * 64 * 4
+    for f in (afno.afno_linear_forward_workspace, afno.afno_linear_backward_workspace):
+        assert f(9000, 512, 512, BF16, 0) > f(9000, 512, 512, BF16, 1)
+        assert f(9000, 513, 512, BF16, 1) >= 9000 * 520 * 2
 
 
 def test_python_refusals():
