@@ -38,12 +38,13 @@ int check_dtype(int dtype) {
              : fail(AFNO_ERR_INVALID_ARG, "dtype must be AFNO_DTYPE_FP32 (0) or AFNO_DTYPE_BF16 (1)");
 }
 
-// rows x cols values that the kernels index with 64 bits and cut into at most 2^31 - 1 workgroups
+// The kernels index with 64 bits; a launch has at most 2^32 threads, which these limits keep: a wave a row of
+// a norm, 256 threads a tile of 64 x 64, a thread eight values.
+constexpr int64_t kMaxWidth = (int64_t)1 << 20, kMaxRows = (int64_t)1 << 26, kMaxValues = (int64_t)1 << 35;
 int check_size(int64_t rows, int64_t cols) {
-  if (cols > (int64_t)1 << 20)
-    return fail(AFNO_ERR_UNSUPPORTED, "more than 2^20 channels");
-  if (rows > 0x7fffffffll || (double)(rows / 64 + 1) * (double)(cols / 64 + 1) > 2.0e9)
-    return fail(AFNO_ERR_UNSUPPORTED, "tensor too large");
+  if (cols > kMaxWidth) return fail(AFNO_ERR_UNSUPPORTED, "more than 2^20 channels");
+  if (rows > kMaxRows) return fail(AFNO_ERR_UNSUPPORTED, "more than 2^26 rows");
+  if (rows > kMaxValues / cols) return fail(AFNO_ERR_UNSUPPORTED, "more than 2^35 values");
   return AFNO_OK;
 }
 
@@ -225,7 +226,7 @@ int run_dropout(const void* x, const void* residual, int64_t n, float p, uint64_
   AFNO_TRY(make_drop(p, seed, offset, counter, &a.drop));
   if (n == 0) return AFNO_OK;
   if (!x || !out) return fail(AFNO_ERR_INVALID_ARG, "null pointer argument");
-  if (n > (int64_t)1 << 41) return fail(AFNO_ERR_UNSUPPORTED, "tensor too large");
+  if (n > kMaxValues) return fail(AFNO_ERR_UNSUPPORTED, "more than 2^35 values");
   const size_t es = dtype == AFNO_DTYPE_FP32 ? 4 : 2;
   AFNO_TRY(check_aligned({x, residual, out}, es));
   AFNO_TRY(check_overlap({{x, n * es}, {residual, n * es}, {counter, 8}}, {{out, n * es}}));

@@ -47,10 +47,13 @@ struct Cut {
 // bf16: 256 where most CUs get a tile of it, also by a split of k that leaves 2,048 to each (64,800 k's, 1,024
 // x 4,096: 520 us in four splits of 256 against 693 in two of 128; 1,080 x 1,536 x 768, 30 tiles: 20 against
 // 8 with 64).  Both: 128 where every CU gets one (bf16, 4,096 x 1,024 x 1,024, 256 tiles: 16.5 us, 64
-// 16.6; 10,368 x 1,536 x 384, 972 tiles: 22 and 32), or by splits of long sums (8,192 k's in 384 x 1,536:
-// 35 us in eight of 128, 41 with 64 whole).  Else 64, split where the tiles leave CUs without one and the sum
-// is long: a split costs the join's launch, about 3 us, and a stage of 64 k's 0.2 us (256 x 1,024 x
-// 4,096, 64 tiles: 16.6 us whole, 13.0 in four; 64 x 4,096 x 1,024: 6.3 whole, 8.7 in two).
+// 16.6; 10,368 x 1,536 x 384, 972 tiles: 22 and 32; fp32 from three in four: 10,368 x 384 x 1,536, 243
+// tiles: 116 and 122), or by splits of long sums (bf16, 10,368 k's in 384 x 1,536: 35 us in eight of 128, 41
+// with 64 whole), in fp32 two to a CU where 2,048 k's are left to each (20,000 k's, 2,048 x 2,048: 1,291 us
+// in two splits, 1,549 whole; but 10,368 k's in 384 x 1,536: 123 in seven, 152 in ten).
+// Else 64, split where the tiles leave CUs without one and the sum is long: a split costs the join's launch,
+// about 3 us, and a stage of k's 0.2 us, in fp32 0.7 (bf16, 256 x 1,024 x 4,096, 64 tiles: 16.6 us whole,
+// 13.0 in four; 64 x 4,096 x 1,024: 6.3 whole, 8.7 in two; fp32 23.7 whole, 12.9 in four).
 // Without units every k-stage waits for its loads: splits until there are two workgroups a CU.
 Cut cut_product(int64_t M, int64_t N, int64_t K, int es, bool units) {
   Cut c;
@@ -73,8 +76,12 @@ Cut cut_product(int64_t M, int64_t N, int64_t K, int es, bool units) {
     const int64_t s = tiles(256) >= 128 ? 1 : fill(tiles(256), 256, 2048);
     if (tiles(256) * s >= 128) return cut(256, s);
   }
-  if (tiles(128) >= 256) return cut(128, 1);
-  if (K >= 8192 && M > 64 && N > 64) return cut(128, fill(tiles(128), 288, 1024));
+  const int64_t t128 = tiles(128);
+  if (K >= 8192 && M > 64 && N > 64 && t128 < 512) {
+    const bool two = es == 4 && 512 / t128 >= 1 && K / (512 / t128) >= 2048;
+    return cut(128, fill(t128, two ? 512 : 256, 1024));
+  }
+  if (t128 >= 256 || (es == 4 && t128 >= 192)) return cut(128, 1);
   return cut(64, tiles(64) >= 256 ? 1 : fill(tiles(64), 256, es == 2 ? 1024 : 256));
 }
 size_t part_of(int64_t M, int64_t N, const Cut& c) {
@@ -90,8 +97,7 @@ size_t part_bytes(int64_t M, int64_t N, int64_t K, int dtype) {
 }
 
 template <typename T, bool AR, bool BR>
-void run_reg(const GemmArgs<T>& g, int tile, int splits, hipStream_t st) {
-  const dim3 grid((unsigned)(8 * ceil_div(ceil_div(g.M, tile) * ceil_div(g.N, tile), 8)), (unsigned)splits);
+void run_reg(const GemmArgs<T>& g, int tile, const dim3& grid, hipStream_t st) {
   constexpr int lds128 = RegGeo<T, AR, BR, 128, 128>::kBytes, lds64 = RegGeo<T, AR, BR, 64, 64>::kBytes;
   if (tile == 128) hipLaunchKernelGGL((gemm_reg<T, AR, BR, 128, 128>), grid, dim3(256), lds128, st, g);
   else hipLaunchKernelGGL((gemm_reg<T, AR, BR, 64, 64>), grid, dim3(256), lds64, st, g);
@@ -115,7 +121,8 @@ hipError_t product(GemmArgs<T> g, float* part, hipStream_t st) {
   const bool units = g.lda % UE == 0 && g.ldb % UE == 0 && at16(g.a) && at16(g.b) &&
                      (!AR || g.ma % UE == 0) && (!BR || g.nb % UE == 0);
   const Cut c = cut_product(g.M, g.N, g.K, (int)sizeof(T), units);
-  const dim3 grid((unsigned)(8 * ceil_div(ceil_div(g.M, c.tile) * ceil_div(g.N, c.tile), 8)), (unsigned)c.splits);
+  const dim3 grid((unsigned)(8 * ceil_div(c.splits * ceil_div(g.M, c.tile) * ceil_div(g.N, c.tile), 8)));
+  g.splits = c.splits;
   g.kper = c.kper;
   g.part = c.splits > 1 ? part : nullptr;
   if (c.tile == 256) {
@@ -124,7 +131,7 @@ hipError_t product(GemmArgs<T> g, float* part, hipStream_t st) {
     if (c.tile == 128) hipLaunchKernelGGL((gemm_tile<T, AR, BR, 128>), grid, dim3(256), 0, st, g);
     else hipLaunchKernelGGL((gemm_tile<T, AR, BR, 64>), grid, dim3(256), 0, st, g);
   } else {
-    run_reg<T, AR, BR>(g, c.tile, c.splits, st);
+    run_reg<T, AR, BR>(g, c.tile, grid, st);
   }
   if (c.splits > 1)
     hipLaunchKernelGGL((join_splits<T>), dim3((unsigned)ceil_div(g.M * ceil_div(g.N, 4), 256)),

@@ -47,11 +47,12 @@ struct Drop {
     }
     return make_uint4(x0, x1, x2, x3);
   }
-  // a value with number j of a group's words
+  // a value with number j of a group's words.  The upper half of a word is compared in place: it is at least
+  // the threshold exactly where the word is at least the threshold's 65,536 fold.
   __device__ __forceinline__ float apply(float v, const uint4& w, int j) const {
     const uint32_t u = j < 2 ? w.x : (j < 4 ? w.y : (j < 6 ? w.z : w.w));
-    const uint32_t r = j & 1 ? u >> 16 : u & 0xffffu;
-    return r >= threshold ? v * scale : 0.f;
+    const bool keep = j & 1 ? u >= threshold << 16 : (uint16_t)u >= (uint16_t)threshold;
+    return keep ? v * scale : 0.f;
   }
   // NV <= 8 neighbouring values from flat index e on, whose numbers may lie in two groups
   template <int NV>

@@ -31,7 +31,8 @@ struct GemmArgs {
   int64_t lda, ldb;   // elements from one row (k for row-major operands) to the next
   int64_t M, N, K;
   int64_t ma, nb;     // rows of a and b that are there to be read: M and N, or rounded up to a unit
-  int64_t kper;       // k of one split, a multiple of the k-stage; splits = gridDim.y
+  int64_t kper;       // k of one split, a multiple of the k-stage
+  int splits;
   float* part;        // [splits][M][N] sums (splits > 1), else null
   Epilogue<T> e;
 };
@@ -146,15 +147,24 @@ __device__ __forceinline__ void load_bias(const Epilogue<T>& e, int64_t N, int64
   for (int j = 0; j < NV; ++j) b[j] = e.bias && n + j < N ? ld_f(e.bias + n + j) : 0.f;
 }
 
-// workgroup -> (tile row, tile column): workgroup g runs on XCD g % 8, and the workgroups of one XCD
-// take neighbouring tiles, column tiles first, so that a row tile's operand stays in that XCD's L2
-__device__ __forceinline__ bool tile_of(int64_t ntile, int nbn, int64_t* mb, int* nb) {
-  const int64_t per = (ntile + 7) / 8, g = blockIdx.x, t = (g & 7) * per + (g >> 3);
-  if ((g >> 3) >= per || t >= ntile) return false;
-  *mb = t / nbn;
-  *nb = (int)(t - *mb * nbn);
-  return true;
-}
+// Workgroup -> split, tile row and tile column, of 8 ceil(splits tiles / 8) workgroups: workgroup g runs on XCD
+// g % 8, and the workgroups of one XCD take neighbouring ones, column tiles first, then rows, then splits, so
+// that a row tile's operand stays in that XCD's L2 and no XCD has more than its eighth (252 workgroups dealt by
+// tile alone left one XCD with 7 and the others with 35 for 32 CUs: 192 us where 108).
+struct TilePlace {
+  int64_t m, n;
+  int split;
+  bool any;
+  __device__ __forceinline__ TilePlace(int64_t rows, int64_t cols, int splits) {
+    const int64_t tiles = rows * cols, all = tiles * splits;
+    const int64_t per = (all + 7) / 8, g = blockIdx.x, t = (g & 7) * per + (g >> 3);
+    any = (g >> 3) < per && t < all;
+    split = (int)(t / tiles);
+    const int64_t i = t - split * tiles;
+    m = i / cols;
+    n = i - m * cols;
+  }
+};
 
 // One 16-byte unit (UE elements along the operand's fastest index) in registers.
 template <typename T> struct Unit {
@@ -213,12 +223,10 @@ __global__ void __launch_bounds__(256) gemm_reg(GemmArgs<T> g) {
   constexpr int BK = G::BK, UE = G::UE, TM = BM / 32, TN = BN / 32;
   extern __shared__ uint4 reg_smem[];
   T* S = reinterpret_cast<T*>(reg_smem);
-  const int nbn = (int)((g.N + BN - 1) / BN);
-  int64_t mb;
-  int nb;
-  if (!tile_of((g.M + BM - 1) / BM * nbn, nbn, &mb, &nb)) return;
-  const int64_t m0 = mb * BM, n0 = (int64_t)nb * BN;
-  const int64_t k0 = blockIdx.y * g.kper, k1 = min(g.K, k0 + g.kper);
+  const TilePlace t((g.M + BM - 1) / BM, (g.N + BN - 1) / BN, g.splits);
+  if (!t.any) return;
+  const int64_t m0 = t.m * BM, n0 = t.n * BN;
+  const int64_t k0 = t.split * g.kper, k1 = min(g.K, k0 + g.kper);
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, gq = lane >> 4;
   const int wm = (tid >> 6) >> 1, wn = (tid >> 6) & 1;
 
@@ -344,7 +352,7 @@ __global__ void __launch_bounds__(256) gemm_reg(GemmArgs<T> g) {
       if (n >= g.N) continue;
       float v[4] = {acc[a][b][0], acc[a][b][1], acc[a][b][2], acc[a][b][3]};
       if (g.part) {
-        float* p = g.part + (blockIdx.y * g.M + m) * g.N + n;
+        float* p = g.part + (t.split * g.M + m) * g.N + n;
         if (g.N % 4 == 0) {
           *reinterpret_cast<float4*>(p) = make_float4(v[0], v[1], v[2], v[3]);
         } else {

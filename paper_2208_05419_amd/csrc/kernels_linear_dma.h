@@ -19,14 +19,25 @@ union DmaOp {
   bf16x8 v;
   float f[4];
 };
-template <typename T>
-__device__ __forceinline__ f32x4 dma_mma(const DmaOp& a, const DmaOp& b, f32x4 c) {
+// acc += the products of a k-half's operands, transposed.  The four fp32 instructions of a tile are spread
+// over the tiles, so that none waits for the one before it.
+template <typename T, int TM, int TN, int AM>
+__device__ __forceinline__ void dma_products(const DmaOp (&fa)[TM], const DmaOp (&fb)[TN], f32x4 (&acc)[AM][TN],
+                                             int a0) {
   if constexpr (sizeof(T) == 2) {
-    return __builtin_amdgcn_mfma_f32_16x16x32_bf16(a.v, b.v, c, 0, 0, 0);
+#pragma unroll
+    for (int a = 0; a < TM; ++a)
+#pragma unroll
+      for (int b = 0; b < TN; ++b)
+        acc[a0 + a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fb[b].v, fa[a].v, acc[a0 + a][b], 0, 0, 0);
   } else {
 #pragma unroll
-    for (int q = 0; q < 4; ++q) c = __builtin_amdgcn_mfma_f32_16x16x4f32(a.f[q], b.f[q], c, 0, 0, 0);
-    return c;
+    for (int q = 0; q < 4; ++q)
+#pragma unroll
+      for (int a = 0; a < TM; ++a)
+#pragma unroll
+        for (int b = 0; b < TN; ++b)
+          acc[a0 + a][b] = __builtin_amdgcn_mfma_f32_16x16x4f32(fb[b].f[q], fa[a].f[q], acc[a0 + a][b], 0, 0, 0);
   }
 }
 
@@ -159,7 +170,7 @@ struct Slab {
 // bytes of 16 rows.  m0, n0: the wave's first row and column.
 template <typename T, bool BR, int TM, int TN>
 __device__ __forceinline__ void dma_store(const GemmArgs<T>& g, const f32x4 (&acc)[TM][TN], int64_t m0,
-                                          int64_t n0, int lane) {
+                                          int64_t n0, int split, int lane) {
   constexpr int NV = 16 / sizeof(T), PER = NV / 4;
   const int l16 = lane & 15, gq = lane >> 4;
   const Drop d(g.e.drop);
@@ -192,7 +203,7 @@ __device__ __forceinline__ void dma_store(const GemmArgs<T>& g, const f32x4 (&ac
         finish_some(g.e, d, g.N, m, n, bv, o, units);
         continue;
       }
-      float* p = g.part + (blockIdx.y * g.M + m) * g.N + n;
+      float* p = g.part + (split * g.M + m) * g.N + n;
       if (g.N % 4 == 0) {
 #pragma unroll
         for (int i = 0; i < PER; ++i)
@@ -225,12 +236,10 @@ __global__ void __launch_bounds__(512) gemm_tile256(GemmArgs<bf16> g) {
   constexpr int BK = 64;
   __shared__ uint4 st0[SA::U + SB::U];
   __shared__ uint4 st1[SA::U + SB::U];
-  const int nbn = (int)((g.N + 255) / 256);
-  int64_t mb;
-  int nb;
-  if (!tile_of((g.M + 255) / 256 * nbn, nbn, &mb, &nb)) return;
-  const int64_t m0 = mb * 256, n0 = (int64_t)nb * 256;
-  const int64_t k0 = blockIdx.y * g.kper, k1 = min(g.K, k0 + g.kper);
+  const TilePlace t((g.M + 256 - 1) / 256, (g.N + 256 - 1) / 256, g.splits);
+  if (!t.any) return;
+  const int64_t m0 = t.m * 256, n0 = t.n * 256;
+  const int64_t k0 = t.split * g.kper, k1 = min(g.K, k0 + g.kper);
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 2, wn = wave & 3;
   const int S = (int)((k1 - k0) / BK);  // whole stages
@@ -266,10 +275,7 @@ __global__ void __launch_bounds__(512) gemm_tile256(GemmArgs<bf16> g) {
       if (q == 3) __builtin_amdgcn_s_waitcnt(kWaitAll);
       dma_barrier();
       __builtin_amdgcn_s_setprio(1);
-#pragma unroll
-      for (int a = 0; a < 4; ++a)
-#pragma unroll
-        for (int b = 0; b < 4; ++b) acc[a0 + a][b] = dma_mma<bf16>(fb[b], fa[a], acc[a0 + a][b]);
+      dma_products<bf16>(fa, fb, acc, a0);
       __builtin_amdgcn_s_setprio(0);
       dma_barrier();
     }
@@ -302,7 +308,7 @@ __global__ void __launch_bounds__(512) gemm_tile256(GemmArgs<bf16> g) {
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(wait_loads(0));
   asm volatile("" ::: "memory");
-  dma_store<bf16, BR, 8, 4>(g, acc, m0 + 128 * wm, n0 + 64 * wn, lane);
+  dma_store<bf16, BR, 8, 4>(g, acc, m0 + 128 * wm, n0 + 64 * wn, t.split, lane);
 }
 
 // Workgroup tile TILE x TILE (128 or 64), 4 waves as 2 x 2, for sizes that give the large tile too few
@@ -320,12 +326,10 @@ __global__ void __launch_bounds__(256) gemm_tile(GemmArgs<T> g) {
   __shared__ uint4 st1[U];
   __shared__ uint4 st2[NS == 4 ? U : 1];
   __shared__ uint4 st3[NS == 4 ? U : 1];
-  const int nbn = (int)((g.N + TILE - 1) / TILE);
-  int64_t mb;
-  int nb;
-  if (!tile_of((g.M + TILE - 1) / TILE * nbn, nbn, &mb, &nb)) return;
-  const int64_t m0 = mb * TILE, n0 = (int64_t)nb * TILE;
-  const int64_t k0 = blockIdx.y * g.kper, k1 = min(g.K, k0 + g.kper);
+  const TilePlace t((g.M + TILE - 1) / TILE, (g.N + TILE - 1) / TILE, g.splits);
+  if (!t.any) return;
+  const int64_t m0 = t.m * TILE, n0 = t.n * TILE;
+  const int64_t k0 = t.split * g.kper, k1 = min(g.K, k0 + g.kper);
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
   const int S = (int)((k1 - k0) / BK);  // whole stages
@@ -351,10 +355,7 @@ __global__ void __launch_bounds__(256) gemm_tile(GemmArgs<T> g) {
       for (int b = 0; b < NTL; ++b) fb[b] = sb.read(st + SA::U, ks, b);
 #pragma unroll
       for (int a = 0; a < NTL; ++a) fa[a] = sa.read(st, ks, a);
-#pragma unroll
-      for (int a = 0; a < NTL; ++a)
-#pragma unroll
-        for (int b = 0; b < NTL; ++b) acc[a][b] = dma_mma<T>(fb[b], fa[a], acc[a][b]);
+      dma_products<T>(fa, fb, acc, 0);
     }
   };
   // this wave's loads of the present stage there (the later ones may be under way), its reads of the last
@@ -416,7 +417,7 @@ __global__ void __launch_bounds__(256) gemm_tile(GemmArgs<T> g) {
     sync_all();
     compute(rest);
   }
-  dma_store<T, BR, NTL, NTL>(g, acc, m0 + WT * wm, n0 + WT * wn, lane);
+  dma_store<T, BR, NTL, NTL>(g, acc, m0 + WT * wm, n0 + WT * wn, t.split, lane);
 }
 
 }  // namespace afno

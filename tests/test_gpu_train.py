@@ -237,13 +237,20 @@ def test_gelu_slope_over_its_range():
 # ---------------------------------------------------------------- LayerNorm
 
 NORM = [(1, 1), (1, 8), (3, 2), (7, 64), (130, 333), (65, 768), (33, 1024), (9, 2048), (1000, 96), (5, 2049), (70, 5000),
-        (2, 8192), (4100, 24)]
+        (2, 8192), (4100, 24), (3, 9001), (1500, 3000)]
 
 
 def norm_slack(v, rstd, C):
     """How far (v - mean) rstd may be off, relative to 1 + its size: v is exact, its mean off by k(C) u of the
     largest value, the variance likewise twice."""
     return 2 * k(C) * U * (1.0 + np.abs(v).max(-1, keepdims=True) * rstd)
+
+
+def norm_dx_slack(a, hh, rstd, e):
+    """How far dx may be off for a = |g gamma|, h = |(v - mean) rstd| and e of norm_slack: each of its terms by e
+    of itself, and h by e (1 + h) wherever it stands."""
+    m = lambda t: t.mean(-1, keepdims=True)  # noqa: E731
+    return 2 * rstd * (e * (a + m(a) + hh * m(a * hh)) + e * (1 + hh) * m(a * hh) + hh * m(a * e * (1 + hh)))
 
 
 @pytest.mark.parametrize("dtype", ["fp32", "bf16"])
@@ -283,10 +290,7 @@ def check_norm(M, C, residual, dtype, put, mean=0.5):
     torch.cuda.synchronize()
     dx, dga, dbe = ot.layer_norm_backward(g, v, ga, eps, res)
     a = np.abs(g * ga)
-    m = lambda t: t.mean(-1, keepdims=True)  # noqa: E731
-    terms = a + m(a) + hh * m(a * hh)
-    tol = 2 * rstd * (e * terms + e * (1 + hh) * m(a * hh) + hh * m(a * e * (1 + hh)))
-    close("dx", d["dx"], dx, tol + 2 * U * np.abs(res) + h * np.abs(dx) * 1.01)
+    close("dx", d["dx"], dx, norm_dx_slack(a, hh, rstd, e) + 2 * U * np.abs(res) + h * np.abs(dx) * 1.01)
     close("dgamma", d["dgamma"], dga, (np.abs(g) * e * (1 + hh) + k(M) * U * np.abs(g) * hh).sum(0))
     close("dbeta", d["dbeta"], dbe, k(M) * U * np.abs(g).sum(0))
 
@@ -353,6 +357,55 @@ def test_one_mask_everywhere():
             assert ((out > 0).cpu().numpy() == want).all() and torch.equal(out, alone)
             s = want.sum(0) * scale_of(0.4)
             assert (np.abs(to_f64(db) - s) <= (2.0 ** -8 if dt == torch.bfloat16 else k(M) * U) * s * 1.01).all()
+
+
+# ---------------------------------------------------------------- beyond 32 bits
+
+def test_offsets_beyond_32_bits():
+    """Tensors of over 2^31 values, checked in their last rows (the first are those of any other test)."""
+    bf = torch.bfloat16
+    gen = torch.Generator(device="cuda")
+    gen.manual_seed(5)
+    n = 2 ** 31 + 12345
+    x = torch.empty(n, dtype=bf, device="cuda")
+    x.fill_(1.0)
+    x[-4096:] = torch.randn(4096, generator=gen, device="cuda").to(bf)
+    tail = afno.dropout_forward(x, 0.3, SEED, offset=OFFSET)[-4096:]
+    want = np.where(keep_from(n - 4096, 4096, 0.3), to_f64(x[-4096:]) * scale_of(0.3), 0.0)
+    close("dropout", tail, want, 2.0 ** -8 * 1.01 * np.abs(want))
+    del x
+    M, K, N = 1_050_000, 16, 2056
+    x = torch.randn(M, K, generator=gen, device="cuda").to(bf)
+    w = torch.randn(K, N, generator=gen, device="cuda").to(bf)
+    out = afno.linear_forward(x, w)
+    ref = to_f64(x[-300:]) @ to_f64(w)
+    close("linear", out[-300:], ref, k(K) * U * (np.abs(to_f64(x[-300:])) @ np.abs(to_f64(w))) + 2.0 ** -8 * np.abs(ref) * 1.01)
+    d = afno.linear_backward(out, x, w, need_dw=False, bias=False)
+    g = to_f64(out[-300:])
+    close("dx", d["dx"][-300:], g @ to_f64(w).T, k(N) * U * (np.abs(g) @ np.abs(to_f64(w)).T) + 2.0 ** -8 * np.abs(g @ to_f64(w).T) * 1.01)
+    ga, be = torch.ones(N, dtype=bf, device="cuda"), torch.zeros(N, dtype=bf, device="cuda")
+    y = afno.layer_norm_forward(out, ga, be)
+    ref = ot.layer_norm(g, 1.0, 0.0, 1e-6)
+    rstd = 1 / g.std(-1, keepdims=True)
+    close("norm", y[-300:], ref, norm_slack(g, rstd, N) * (1 + np.abs(ref)) + 2.0 ** -8 * np.abs(ref) * 1.01)
+    del y
+    up = torch.zeros_like(out)
+    up[-300:] = torch.randn(300, N, generator=gen, device="cuda").to(bf)
+    dx = afno.layer_norm_backward(up, out, ga)["dx"]
+    u64 = to_f64(up[-300:])
+    ref = ot.layer_norm_backward(u64, g, 1.0, 1e-6)[0]
+    hh = np.abs(ot.layer_norm(g, 1.0, 0.0, 1e-6))
+    close("norm dx", dx[-300:], ref, norm_dx_slack(np.abs(u64), hh, rstd, norm_slack(g, rstd, N)) + 2.0 ** -8 * np.abs(ref) * 1.01)
+
+
+def keep_from(first, n, p):
+    """ot.keep of the n elements from `first` on."""
+    i = np.arange(first // 8, (first + n) // 8 + 1, dtype=np.uint64)
+    full = lambda v: np.full(i.shape, v, dtype=np.uint64)  # noqa: E731
+    words = ot.philox4x32((i & ot.LOW, i >> ot.HALF, full(OFFSET & 0xFFFFFFFF), full(OFFSET >> 32)),
+                          (SEED & 0xFFFFFFFF, SEED >> 32), 7)
+    numbers = np.stack([v for w in words for v in (w & np.uint64(0xFFFF), w >> np.uint64(16))], axis=-1)
+    return numbers.reshape(-1)[first % 8:first % 8 + n] >= ot.threshold(p)
 
 
 # ---------------------------------------------------------------- together, streams, graphs
