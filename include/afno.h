@@ -235,7 +235,7 @@ int afno_filter_backward(const void* x, const void* w1, const void* b1, const vo
  * the rest of an AFNO block (LayerNorm, the channel MLP, the residual adds) as operators of their
  * own.  Arrays are rows of channels, [M][C] with the channels fastest (a [B][H][W][C] grid: M = B H W),
  * contiguous device memory on the current device, aligned to their element (16 bytes take the wider
- * kernels).  Any M from 0 to 2^26, any width up to 2^20, up to 2^35 values an array
+ * kernels).  Any M from 0 to 2^25, any width up to 2^20, up to 2^34 values an array
  * (AFNO_ERR_UNSUPPORTED beyond).  No output may overlap an input or another output (AFNO_ERR_ALIAS).  Ownership, asynchrony and errors as
  * afno_filter_forward; sums are held in float32 and added in a fixed order, so repeated calls give
  * the same bits.

@@ -40,11 +40,11 @@ int check_dtype(int dtype) {
 
 // The kernels index with 64 bits; a launch has at most 2^32 threads, which these limits keep: a wave a row of
 // a norm, 256 threads a tile of 64 x 64, a thread eight values.
-constexpr int64_t kMaxWidth = (int64_t)1 << 20, kMaxRows = (int64_t)1 << 26, kMaxValues = (int64_t)1 << 35;
+constexpr int64_t kMaxWidth = (int64_t)1 << 20, kMaxRows = (int64_t)1 << 25, kMaxValues = (int64_t)1 << 34;
 int check_size(int64_t rows, int64_t cols) {
   if (cols > kMaxWidth) return fail(AFNO_ERR_UNSUPPORTED, "more than 2^20 channels");
-  if (rows > kMaxRows) return fail(AFNO_ERR_UNSUPPORTED, "more than 2^26 rows");
-  if (rows > kMaxValues / cols) return fail(AFNO_ERR_UNSUPPORTED, "more than 2^35 values");
+  if (rows > kMaxRows) return fail(AFNO_ERR_UNSUPPORTED, "more than 2^25 rows");
+  if (rows > kMaxValues / cols) return fail(AFNO_ERR_UNSUPPORTED, "more than 2^34 values");
   return AFNO_OK;
 }
 
@@ -82,10 +82,6 @@ int check_workspace(const void* ws, int64_t have, size_t need, std::initializer_
 // graph, was not there for its last reader in a replay.
 template <typename F>
 int with_workspace(void* given, size_t bytes, hipStream_t stream, F launch) {
-  std::call_once(g_attr_once, [] {
-    (void)afno::set_kernel_attributes();
-    (void)hipGetLastError();
-  });
   if (given || !bytes) {
     const hipError_t e = launch(given);
     return e == hipSuccess ? AFNO_OK : fail(AFNO_ERR_HIP, std::string("launch: ") + hipGetErrorString(e));
@@ -226,7 +222,7 @@ int run_dropout(const void* x, const void* residual, int64_t n, float p, uint64_
   AFNO_TRY(make_drop(p, seed, offset, counter, &a.drop));
   if (n == 0) return AFNO_OK;
   if (!x || !out) return fail(AFNO_ERR_INVALID_ARG, "null pointer argument");
-  if (n > kMaxValues) return fail(AFNO_ERR_UNSUPPORTED, "more than 2^35 values");
+  if (n > kMaxValues) return fail(AFNO_ERR_UNSUPPORTED, "more than 2^34 values");
   const size_t es = dtype == AFNO_DTYPE_FP32 ? 4 : 2;
   AFNO_TRY(check_aligned({x, residual, out}, es));
   AFNO_TRY(check_overlap({{x, n * es}, {residual, n * es}, {counter, 8}}, {{out, n * es}}));
@@ -239,7 +235,7 @@ int run_dropout(const void* x, const void* residual, int64_t n, float p, uint64_
 const void* some_address(int aligned) { return reinterpret_cast<const void*>((uintptr_t)(aligned ? 16 : 4)); }
 
 template <typename F>
-int64_t workspace_of(int64_t M, int64_t K, int64_t N, int dtype, F bytes) {
+int64_t workspace_of(int64_t M, int64_t K, int64_t N, int dtype, F bytes) noexcept try {
   g_last_error.clear();
   int rc = check_dtype(dtype);
   if (rc == AFNO_OK && (M < 0 || K <= 0 || N <= 0)) rc = fail(AFNO_ERR_INVALID_ARG, "sizes must be positive");
@@ -248,6 +244,8 @@ int64_t workspace_of(int64_t M, int64_t K, int64_t N, int dtype, F bytes) {
   if (rc == AFNO_OK) rc = check_size(K, N);
   if (rc != AFNO_OK) return rc;
   return M ? (int64_t)bytes() : 0;
+} catch (...) {
+  return AFNO_ERR_HIP;
 }
 
 // no C++ exception (of an allocation for an error's text, of a mutex) passes a C entry

@@ -30,7 +30,6 @@
 #include "afno_rows.hip"
 #include "afno_train.hip"
 #endif
-#include "train_internal.h"
 #include "kernels_fast.h"
 #include "kernels_generic.h"
 #include "kernels_mfma.h"
@@ -666,7 +665,7 @@ hipError_t launch_block(const Plan& pl, const BlockPtrs& a, hipStream_t st) {
 
 hipError_t set_kernel_attributes() {
   const int lds_max = kLdsBytes;
-  hipError_t e, first = set_train_attributes();
+  hipError_t e, first = hipSuccess;
 #define AFNO_ATTR(K)                                                                         \
   e = hipFuncSetAttribute(reinterpret_cast<const void*>(K),                                \
                           hipFuncAttributeMaxDynamicSharedMemorySize, lds_max);            \

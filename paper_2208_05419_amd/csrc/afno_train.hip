@@ -96,13 +96,6 @@ size_t part_bytes(int64_t M, int64_t N, int64_t K, int dtype) {
   return std::max(part_of(M, N, cut_product(M, N, K, es, false)), part_of(M, N, cut_product(M, N, K, es, true)));
 }
 
-template <typename T, bool AR, bool BR>
-void run_reg(const GemmArgs<T>& g, int tile, const dim3& grid, hipStream_t st) {
-  constexpr int lds128 = RegGeo<T, AR, BR, 128, 128>::kBytes, lds64 = RegGeo<T, AR, BR, 64, 64>::kBytes;
-  if (tile == 128) hipLaunchKernelGGL((gemm_reg<T, AR, BR, 128, 128>), grid, dim3(256), lds128, st, g);
-  else hipLaunchKernelGGL((gemm_reg<T, AR, BR, 64, 64>), grid, dim3(256), lds64, st, g);
-}
-
 // One product with its epilogue; part: room for part_bytes.  Operands at any address and stride: the
 // direct-to-LDS kernels where both are 16-byte units, else gemm_reg.
 template <typename T, bool AR, bool BR>
@@ -128,10 +121,11 @@ hipError_t product(GemmArgs<T> g, float* part, hipStream_t st) {
   if (c.tile == 256) {
     if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((gemm_tile256<AR, BR>), grid, dim3(512), 0, st, g);
   } else if (units) {
-    if (c.tile == 128) hipLaunchKernelGGL((gemm_tile<T, AR, BR, 128>), grid, dim3(256), 0, st, g);
-    else hipLaunchKernelGGL((gemm_tile<T, AR, BR, 64>), grid, dim3(256), 0, st, g);
+    if (c.tile == 128) hipLaunchKernelGGL((gemm_tile<T, AR, BR, 128>), grid, dim3(TileWaves<T>::NT), 0, st, g);
+    else hipLaunchKernelGGL((gemm_tile<T, AR, BR, 64>), grid, dim3(TileWaves<T>::NT), 0, st, g);
   } else {
-    run_reg<T, AR, BR>(g, c.tile, grid, st);
+    if (c.tile == 128) hipLaunchKernelGGL((gemm_reg<T, AR, BR, 128, 128>), grid, dim3(256), 0, st, g);
+    else hipLaunchKernelGGL((gemm_reg<T, AR, BR, 64, 64>), grid, dim3(256), 0, st, g);
   }
   if (c.splits > 1)
     hipLaunchKernelGGL((join_splits<T>), dim3((unsigned)ceil_div(g.M * ceil_div(g.N, 4), 256)),
@@ -153,7 +147,9 @@ template <typename T>
 void pack(const PackArgs<T>& a, const PackArgs<T>& b, hipStream_t st) {
   constexpr int UE = Unit<T>::UE;
   const int64_t units = a.rows * (a.ld / UE) + b.rows * (b.ld / UE);
-  if (units) hipLaunchKernelGGL((pack_rows<T>), dim3((unsigned)ceil_div(units, 256)), dim3(256), 0, st, a, b);
+  if (units)
+    hipLaunchKernelGGL((pack_rows<T>), dim3((unsigned)std::min<int64_t>(1 << 20, ceil_div(units, 256))), dim3(256),
+                       0, st, a, b);
 }
 int64_t whole_units(int64_t n, int es) { return ceil_div(n, 16 / es) * (16 / es); }
 
@@ -214,24 +210,6 @@ Layout backward_layout(const LinearBwd& a) {
 }
 
 }  // namespace
-
-hipError_t set_train_attributes() {
-  hipError_t first = hipSuccess;
-  auto set = [&](const void* k) {
-    const hipError_t e = hipFuncSetAttribute(k, hipFuncAttributeMaxDynamicSharedMemorySize, 160 * 1024);
-    if (e != hipSuccess && first == hipSuccess) first = e;
-  };
-#define AFNO_REG(T, AR, BR)                                                        \
-  set(reinterpret_cast<const void*>(&gemm_reg<T, AR, BR, 128, 128>));
-  AFNO_REG(float, false, true)
-  AFNO_REG(float, false, false)
-  AFNO_REG(float, true, true)
-  AFNO_REG(bf16, false, true)
-  AFNO_REG(bf16, false, false)
-  AFNO_REG(bf16, true, true)
-#undef AFNO_REG
-  return first;
-}
 
 size_t linear_forward_bytes(const LinearFwd& a) { return forward_layout(a).bytes; }
 

@@ -156,13 +156,14 @@ struct TilePlace {
   int split;
   bool any;
   __device__ __forceinline__ TilePlace(int64_t rows, int64_t cols, int splits) {
-    const int64_t tiles = rows * cols, all = tiles * splits;
-    const int64_t per = (all + 7) / 8, g = blockIdx.x, t = (g & 7) * per + (g >> 3);
+    // (a launch has fewer than 2^31 workgroups)
+    const uint32_t nc = (uint32_t)cols, tiles = (uint32_t)rows * nc, all = tiles * (uint32_t)splits;
+    const uint32_t per = (all + 7) / 8, g = blockIdx.x, t = (g & 7) * per + (g >> 3);
     any = (g >> 3) < per && t < all;
-    split = (int)(t / tiles);
-    const int64_t i = t - split * tiles;
-    m = i / cols;
-    n = i - m * cols;
+    const uint32_t s = t / tiles, i = t - s * tiles, r = i / nc;
+    split = (int)s;
+    m = r;
+    n = i - r * nc;
   }
 };
 
@@ -221,8 +222,8 @@ template <typename T, bool AR, bool BR, int BM, int BN>
 __global__ void __launch_bounds__(256) gemm_reg(GemmArgs<T> g) {
   typedef RegGeo<T, AR, BR, BM, BN> G;
   constexpr int BK = G::BK, UE = G::UE, TM = BM / 32, TN = BN / 32;
-  extern __shared__ uint4 reg_smem[];
-  T* S = reinterpret_cast<T*>(reg_smem);
+  __shared__ uint4 smem[G::kBytes / 16];
+  T* S = reinterpret_cast<T*>(smem);
   const TilePlace t((g.M + BM - 1) / BM, (g.N + BN - 1) / BN, g.splits);
   if (!t.any) return;
   const int64_t m0 = t.m * BM, n0 = t.n * BN;
@@ -543,16 +544,13 @@ struct PackArgs {
 template <typename T>
 __global__ void __launch_bounds__(256) pack_rows(PackArgs<T> a, PackArgs<T> b) {
   constexpr int UE = Unit<T>::UE;
-  int64_t u = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t na = a.rows * (a.ld / UE);
-  const bool second = u >= na;
-  if (second) u -= na;
-  const PackArgs<T> p = second ? b : a;
-  if (!p.rows) return;
-  const int64_t per = p.ld / UE, r = u / per, c = UE * (u - r * per);
-  if (r >= p.rows) return;
-  const uint4 w = Unit<T>::template load<false>(p.src + r * p.cols + c, p.cols - c);
-  *reinterpret_cast<uint4*>(p.dst + r * p.ld + c) = w;
+  const int64_t na = a.rows * (a.ld / UE), all = na + b.rows * (b.ld / UE);
+  for (int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x; i < all; i += (int64_t)gridDim.x * 256) {
+    const PackArgs<T>& p = i < na ? a : b;
+    const int64_t u = i < na ? i : i - na, per = p.ld / UE, r = u / per, c = UE * (u - r * per);
+    const uint4 w = Unit<T>::template load<false>(p.src + r * p.cols + c, p.cols - c);
+    *reinterpret_cast<uint4*>(p.dst + r * p.ld + c) = w;
+  }
 }
 
 // The sums over `chunks` of part[chunk][n], n < N, in an order that does not change: 64 threads of a

@@ -311,16 +311,22 @@ __global__ void __launch_bounds__(512) gemm_tile256(GemmArgs<bf16> g) {
   dma_store<bf16, BR, 8, 4>(g, acc, m0 + 128 * wm, n0 + 64 * wn, t.split, lane);
 }
 
-// Workgroup tile TILE x TILE (128 or 64), 4 waves as 2 x 2, for sizes that give the large tile too few
-// workgroups.  Stages of 32 KB (16 KB) in two (four) LDS buffers, so that two workgroups share a CU and
+// Workgroup tile TILE x TILE (128 or 64), 4 waves as 2 x 2, fp32 8 as 2 x 4 (two to a SIMD cover each other's
+// waits where a CU has one workgroup: 10,368 x 1,536 x 384 126 -> 113 us), for sizes that give the large
+// tile too few workgroups.  Stages of 32 KB (16 KB) in two (four) LDS buffers, so that two workgroups share a CU and
 // cover each other's waits; the small tile's products are short, so its loads go out three stages
 // ahead.  The buffers are separate arrays: the compiler then sees that a buffer being read is not one whose
 // loads are under way.
+template <typename T>
+struct TileWaves {
+  static constexpr int N = sizeof(T) == 4 ? 4 : 2, NT = 128 * N;
+};
 template <typename T, bool AR, bool BR, int TILE>
-__global__ void __launch_bounds__(256) gemm_tile(GemmArgs<T> g) {
-  constexpr int WT = TILE / 2, NTL = WT / 16, NS = TILE == 128 ? 2 : 4;
-  typedef Slab<T, AR, false, TILE, WT, 256> SA;
-  typedef Slab<T, BR, true, TILE, WT, 256> SB;
+__global__ void __launch_bounds__((TileWaves<T>::NT)) gemm_tile(GemmArgs<T> g) {
+  constexpr int WN = TileWaves<T>::N, NT = TileWaves<T>::NT, WR = TILE / 2, WC = TILE / WN;
+  constexpr int TM = WR / 16, TN = WC / 16, NS = TILE == 128 ? 2 : 4;
+  typedef Slab<T, AR, false, TILE, WR, NT> SA;
+  typedef Slab<T, BR, true, TILE, WC, NT> SB;
   constexpr int BK = SA::BK, U = SA::U + SB::U, L = SA::L + SB::L;
   __shared__ uint4 st0[U];
   __shared__ uint4 st1[U];
@@ -331,16 +337,16 @@ __global__ void __launch_bounds__(256) gemm_tile(GemmArgs<T> g) {
   const int64_t m0 = t.m * TILE, n0 = t.n * TILE;
   const int64_t k0 = t.split * g.kper, k1 = min(g.K, k0 + g.kper);
   const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave / WN, wn = wave % WN;
   const int S = (int)((k1 - k0) / BK);  // whole stages
   const SA sa(g.a, g.lda, m0, g.ma, k0, tid, wm);
   const SB sb(g.b, g.ldb, n0, g.nb, k0, tid, wn);
 
-  f32x4 acc[NTL][NTL];
+  f32x4 acc[TM][TN];
 #pragma unroll
-  for (int a = 0; a < NTL; ++a)
+  for (int a = 0; a < TM; ++a)
 #pragma unroll
-    for (int b = 0; b < NTL; ++b) acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+    for (int b = 0; b < TN; ++b) acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
   // stage s (behind the last: that one again, into a buffer nobody reads, so that every wait counts alike)
   auto issue = [&](uint4* st, int s) {
     const int64_t k = (int64_t)min(s, S - 1) * BK;
@@ -350,11 +356,11 @@ __global__ void __launch_bounds__(256) gemm_tile(GemmArgs<T> g) {
   auto compute = [&](const uint4* st) {
 #pragma unroll
     for (int ks = 0; ks < 2; ++ks) {
-      DmaOp fa[NTL], fb[NTL];
+      DmaOp fa[TM], fb[TN];
 #pragma unroll
-      for (int b = 0; b < NTL; ++b) fb[b] = sb.read(st + SA::U, ks, b);
+      for (int b = 0; b < TN; ++b) fb[b] = sb.read(st + SA::U, ks, b);
 #pragma unroll
-      for (int a = 0; a < NTL; ++a) fa[a] = sa.read(st, ks, a);
+      for (int a = 0; a < TM; ++a) fa[a] = sa.read(st, ks, a);
       dma_products<T>(fa, fb, acc, 0);
     }
   };
@@ -417,7 +423,7 @@ __global__ void __launch_bounds__(256) gemm_tile(GemmArgs<T> g) {
     sync_all();
     compute(rest);
   }
-  dma_store<T, BR, NTL, NTL>(g, acc, m0 + WT * wm, n0 + WT * wn, t.split, lane);
+  dma_store<T, BR, TM, TN>(g, acc, m0 + WR * wm, n0 + WC * wn, t.split, lane);
 }
 
 }  // namespace afno

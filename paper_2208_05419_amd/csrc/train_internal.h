@@ -48,7 +48,6 @@ struct DropRunArgs {
   void* out;
 };
 
-hipError_t set_train_attributes();
 // workspace bytes (0: none), and the launches with that much at ws
 size_t linear_forward_bytes(const LinearFwd& a);
 hipError_t launch_linear_forward(const LinearFwd& a, void* ws, hipStream_t st);

@@ -50,8 +50,8 @@ def drop(**kw):
     (linear, INV, dict(act=-1)), (linear, INV, dict(dtype=2)), (linear, INV, dict(p=1.0)),
     (linear, INV, dict(p=-0.1)), (linear, INV, dict(p=math.nan)), (linear, INV, dict(p=1 - 2.0 ** -18)),
     (linear, UNS, dict(x=A[0] + 1)), (linear, UNS, dict(b=A[2] + 1)), (linear, UNS, dict(counter=A[6] + 4)),
-    (linear, UNS, dict(dtype=0, w=A[1] + 2)), (linear, UNS, dict(K=2 ** 20 + 1)), (linear, UNS, dict(M=2 ** 26 + 1)),
-    (linear, UNS, dict(M=2 ** 26, N=1024)), (linear, UNS, dict(M=2 ** 62)), (norm, UNS, dict(M=2 ** 25, C=2048)),
+    (linear, UNS, dict(dtype=0, w=A[1] + 2)), (linear, UNS, dict(K=2 ** 20 + 1)), (linear, UNS, dict(M=2 ** 25 + 1)),
+    (linear, UNS, dict(M=2 ** 25, N=1024)), (linear, UNS, dict(M=2 ** 62)), (norm, UNS, dict(M=2 ** 24, C=2048)),
     (linear, UNS, dict(N=2 ** 21)), (linear, ALI, dict(out=A[0])), (linear, ALI, dict(out=A[1] + 64)),
     (linear, ALI, dict(out=A[3])), (linear, ALI, dict(pre=A[4] + 16 * 32 * 2 - 2)), (linear, ALI, dict(pre=A[2])),
     (linear, ALI, dict(out=A[6])),
@@ -73,7 +73,7 @@ def drop(**kw):
     (linear_bwd, ALI, dict(ws=A[0] - 64, have=1 << 26)), (norm_bwd, INV, dict(ws=A[8], have=8)),
     (norm_bwd, ALI, dict(ws=A[1], have=1 << 26)), (linear, ALI, dict(K=4096, ws=A[0], have=1 << 26)),
     (drop, INV, dict(x=None)), (drop, INV, dict(out=None)), (drop, INV, dict(n=-1)), (drop, INV, dict(p=1.0)),
-    (drop, INV, dict(dtype=7)), (drop, UNS, dict(x=A[0] + 1)), (drop, UNS, dict(n=2 ** 35 + 1)), (drop, UNS, dict(n=2 ** 62)),
+    (drop, INV, dict(dtype=7)), (drop, UNS, dict(x=A[0] + 1)), (drop, UNS, dict(n=2 ** 34 + 1)), (drop, UNS, dict(n=2 ** 62)),
     (drop, ALI, dict(out=A[0])), (drop, ALI, dict(out=A[1] + 4)),
 ])
 def test_refused(call, want, kw):
