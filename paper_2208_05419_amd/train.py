@@ -76,17 +76,28 @@ def _aligned(*addresses) -> bool:
     return all(not a or a % 16 == 0 for a in addresses)
 
 
+def _fit(x, *pairs) -> bool:
+    """Whether _expect would pass: every tensor (or None) of the (tensor, shape) pairs has that shape
+    and x's dtype and device, all are contiguous, and x is on the GPU.  Small calls take about as long as
+    their checks, and this is the quick one; _expect says what is wrong."""
+    dtype, device = x.dtype, x.device
+    for t, shape in pairs:
+        if t is not None and (t.shape != shape or t.dtype != dtype or t.device != device
+                              or not t.is_contiguous()):
+            return False
+    return x.is_contiguous() and x.is_cuda
+
+
 def _rows(name, x):
-    """(M, C) of a tensor seen as rows of channels."""
+    """(M, C, dtype code) of a tensor seen as rows of channels."""
     if x is None:
         raise ValueError(f"{name} is missing")
     if x.dim() < 1:
         raise ValueError(f"{name} must have at least one dimension")
-    _dtype_code(x)
-    C = int(x.shape[-1])
+    code, C = _dtype_code(x), x.shape[-1]
     if C == 0:
         raise ValueError(f"{name} has no channels")
-    return x.numel() // C, C
+    return x.numel() // C, C, code
 
 
 def _activation(activation) -> int:
@@ -97,9 +108,8 @@ def _activation(activation) -> int:
 
 def _random(x, p, seed, offset, counter):
     """Dropout's arguments checked: p, the two 64-bit numbers, the counter's address."""
-    for name, v in (("seed", seed), ("offset", offset)):
-        if not isinstance(v, int) or not 0 <= v < 2 ** 64:
-            raise ValueError(f"{name} must be an int in [0, 2^64), got {v!r}")
+    if not (isinstance(seed, int) and isinstance(offset, int) and 0 <= seed < 2 ** 64 and 0 <= offset < 2 ** 64):
+        raise ValueError(f"seed and offset must be ints in [0, 2^64), got {seed!r} and {offset!r}")
     if counter is not None:
         import torch
         if counter.dtype != torch.int64 or counter.numel() != 1:
@@ -144,10 +154,9 @@ def _bytes(query, *sizes) -> int:
 def _workspace(x, nbytes: int):
     """(address, bytes) of a workspace from torch's allocator, which a captured graph keeps, and the
     tensor that holds it."""
-    import torch
     if nbytes == 0:
         return None, 0, None
-    t = torch.empty(nbytes, dtype=torch.uint8, device=x.device)
+    t = x.new_empty(-(-nbytes // x.element_size()))
     return t.data_ptr(), nbytes, t
 
 
@@ -161,21 +170,18 @@ def linear_forward(x, w, b=None, *, activation="none", residual=None, p=0.0, see
     and offset (+ counter[0], an int64 tensor on x's device that is read when the kernel runs): the
     same numbers give the same mask, so a model gives each of its dropouts an offset range of its own
     and counts its steps in counter.  Enqueued on ``stream`` (default: torch's current stream)."""
-    import torch
-    M, K = _rows("x", x)
+    M, K, code = _rows("x", x)
     if w is None or w.dim() != 2:
         raise ValueError("w must be [K, N]")
-    N = int(w.shape[1])
+    N = w.shape[1]
     shape = (*x.shape[:-1], N)
-    specs = [("w", w, (K, N), None)]
-    specs += [(n, t, s, None) for n, t, s in (("b", b, (N,)), ("residual", residual, shape),
-                                              ("out", out, shape), ("pre", pre, shape)) if t is not None]
-    _expect(x, specs)
+    if not _fit(x, (w, (K, N)), (b, (N,)), (residual, shape), (out, shape), (pre, shape)):
+        _expect(x, [("w", w, (K, N), None)] + [(n, t, s, None) for n, t, s in (
+            ("b", b, (N,)), ("residual", residual, shape), ("out", out, shape), ("pre", pre, shape)) if t is not None])
     act, drop = _activation(activation), _random(x, p, seed, offset, counter)
-    code = _dtype_code(x)
 
     def call(handle):
-        y = torch.empty(shape, dtype=x.dtype, device=x.device) if out is None else out
+        y = x.new_empty(shape) if out is None else out
         px, pw = _address(x), _address(w)
         ws, nbytes, _held = _workspace(x, _bytes(afno_linear_forward_workspace, M, K, N, code,
                                                  _aligned(px, pw)))
@@ -192,31 +198,28 @@ def linear_backward(g, x, w, *, pre=None, activation="none", p=0.0, seed=0, offs
     a dict with dx like x, dw like w, db [N], in x's dtype, None where bias, need_dx or need_dw says
     that it is not wanted.  activation, p, seed, offset and the counter's value as in the forward
     call, pre the tensor that it filled (not read without an activation)."""
-    import torch
-    M, K = _rows("x", x)
+    M, K, code = _rows("x", x)
     if w is None or w.dim() != 2:
         raise ValueError("w must be [K, N]")
-    N = int(w.shape[1])
+    N = w.shape[1]
     act = _activation(activation)
     shape = (*x.shape[:-1], N)
-    specs = [("w", w, (K, N), None), ("g", g, shape, None)]
-    if act:
-        specs.append(("pre", pre, shape, None))
-    _expect(x, specs)
+    if act == AFNO_ACT_NONE:
+        pre = None  # not read
+    if g is None or (act and pre is None) or not _fit(x, (w, (K, N)), (g, shape), (pre, shape)):
+        _expect(x, [("w", w, (K, N), None), ("g", g, shape, None)] + ([("pre", pre, shape, None)] if act else []))
     if not (bias or need_dx or need_dw):
         raise ValueError("no gradient is asked for")
     drop = _random(x, p, seed, offset, counter)
-    code = _dtype_code(x)
 
     def call(handle):
-        dx = torch.empty_like(x) if need_dx else None
-        dw = torch.empty_like(w) if need_dw else None
-        db = torch.empty(N, dtype=x.dtype, device=x.device) if bias else None
+        dx = x.new_empty(x.shape) if need_dx else None
+        dw = x.new_empty((K, N)) if need_dw else None
+        db = x.new_empty(N) if bias else None
         pg, px, pw = _address(g), _address(x), _address(w)
         ws, nbytes, _held = _workspace(x, _bytes(afno_linear_backward_workspace, M, K, N, code,
                                                  _aligned(pg, px, pw)))
-        _check(afno_linear_backward(pg, px, pw, _address(pre) if act else None, M, K, N,
-                                    act, *drop, code, _address(dx), _address(dw), _address(db), ws, nbytes, handle))
+        _check(afno_linear_backward(pg, px, pw, _address(pre), M, K, N, act, *drop, code, _address(dx), _address(dw), _address(db), ws, nbytes, handle))
         return {"dx": dx, "dw": dw, "db": db}
 
     return _launch(x, stream, (g, x, w, pre, counter), call)
@@ -226,16 +229,15 @@ def layer_norm_forward(x, gamma, beta, *, eps=1e-6, residual=None, out=None, sum
     """LayerNorm over the last axis of v = x + residual (rounded to x's dtype; None: v = x):
     (v - mean) / sqrt(var + eps) * gamma + beta with the biased variance.  sum_out: a tensor like x
     that receives v, the residual stream and what layer_norm_backward takes."""
-    import torch
-    M, C = _rows("x", x)
-    specs = [("gamma", gamma, (C,), None), ("beta", beta, (C,), None)]
-    specs += [(n, t, tuple(x.shape), None) for n, t in (("residual", residual), ("out", out),
-                                                         ("sum_out", sum_out)) if t is not None]
-    _expect(x, specs)
-    code = _dtype_code(x)
+    M, C, code = _rows("x", x)
+    shape = x.shape
+    if gamma is None or beta is None or not _fit(x, (gamma, (C,)), (beta, (C,)), (residual, shape), (out, shape),
+                                                 (sum_out, shape)):
+        _expect(x, [("gamma", gamma, (C,), None), ("beta", beta, (C,), None)] + [(n, t, tuple(shape), None) for n, t in (
+            ("residual", residual), ("out", out), ("sum_out", sum_out)) if t is not None])
 
     def call(handle):
-        y = torch.empty_like(x) if out is None else out
+        y = x.new_empty(shape) if out is None else out
         _check(afno_layer_norm_forward(_address(x), _address(residual), _address(gamma), _address(beta), M, C, eps,
                                        code, _address(y), _address(sum_out), handle))
         return y
@@ -248,17 +250,15 @@ def layer_norm_backward(g, x, gamma, *, eps=1e-6, gsum=None, stream=None):
     (x's dtype; gsum, the gradient that reaches v along the residual stream, is added to it) and
     dgamma, dbeta (float32)."""
     import torch
-    M, C = _rows("x", x)
-    specs = [("gamma", gamma, (C,), None), ("g", g, tuple(x.shape), None)]
-    if gsum is not None:
-        specs.append(("gsum", gsum, tuple(x.shape), None))
-    _expect(x, specs)
-    code = _dtype_code(x)
+    M, C, code = _rows("x", x)
+    shape = x.shape
+    if gamma is None or g is None or not _fit(x, (gamma, (C,)), (g, shape), (gsum, shape)):
+        _expect(x, [("gamma", gamma, (C,), None), ("g", g, tuple(shape), None)] + (
+            [] if gsum is None else [("gsum", gsum, tuple(shape), None)]))
 
     def call(handle):
-        dx = torch.empty_like(x)
-        dgamma = torch.empty(C, dtype=torch.float32, device=x.device)
-        dbeta = torch.empty(C, dtype=torch.float32, device=x.device)
+        dx = x.new_empty(shape)
+        dgamma, dbeta = x.new_empty(C, dtype=torch.float32), x.new_empty(C, dtype=torch.float32)
         ws, nbytes, _held = _workspace(x, _bytes(afno_layer_norm_backward_workspace, M, C, code))
         _check(afno_layer_norm_backward(_address(g), _address(x), _address(gamma), _address(gsum), M, C, eps, code,
                                         _address(dx), _address(dgamma), _address(dbeta), ws, nbytes, handle))
@@ -269,14 +269,15 @@ def layer_norm_backward(g, x, gamma, *, eps=1e-6, gsum=None, stream=None):
 
 def dropout_forward(x, p, seed, *, offset=0, counter=None, residual=None, out=None, stream=None):
     """drop(x) + residual for a tensor of any shape; dropout's numbers as in linear_forward."""
-    import torch
-    specs = [(n, t, tuple(x.shape), None) for n, t in (("residual", residual), ("out", out)) if t is not None]
-    code = _dtype_code(x)
-    _expect(x, specs)
+    if x is None:
+        raise ValueError("x is missing")
+    code, shape = _dtype_code(x), x.shape
+    if not _fit(x, (residual, shape), (out, shape)):
+        _expect(x, [(n, t, tuple(shape), None) for n, t in (("residual", residual), ("out", out)) if t is not None])
     drop = _random(x, p, seed, offset, counter)
 
     def call(handle):
-        y = torch.empty_like(x) if out is None else out
+        y = x.new_empty(shape) if out is None else out
         _check(afno_dropout_forward(_address(x), _address(residual), x.numel(), *drop, code, _address(y), handle))
         return y
 
@@ -285,13 +286,15 @@ def dropout_forward(x, p, seed, *, offset=0, counter=None, residual=None, out=No
 
 def dropout_backward(g, p, seed, *, offset=0, counter=None, out=None, stream=None):
     """drop(g), the gradient of dropout_forward's x for g = dL/dout (the residual's is g)."""
-    import torch
-    code = _dtype_code(g)
-    _expect(g, [] if out is None else [("out", out, tuple(g.shape), None)])
+    if g is None:
+        raise ValueError("g is missing")
+    code, shape = _dtype_code(g), g.shape
+    if not _fit(g, (out, shape)):
+        _expect(g, [] if out is None else [("out", out, tuple(shape), None)])
     drop = _random(g, p, seed, offset, counter)
 
     def call(handle):
-        dx = torch.empty_like(g) if out is None else out
+        dx = g.new_empty(shape) if out is None else out
         _check(afno_dropout_backward(_address(g), g.numel(), *drop, code, _address(dx), handle))
         return dx
 
