@@ -68,7 +68,7 @@ __device__ __forceinline__ void dma_barrier() {
 // granule c of row k at c ^ f(k).  bf16 takes an operand with two transposing reads, whose pass is half a
 // wave, eight rows k of 32 bytes (A) or of four pieces of 8 (B): f moves the rows to other granules, and
 // B's odd pieces take the other half of theirs.  fp32 takes it value by value, four rows k of 64 bytes at
-// a time, which f spreads.  No bank conflicts by the counters.
+// a time, which f spreads.  No bank conflicts by the counters, in any tile of either type.
 template <typename T, bool R, bool B, int W, int WAVE, int NT>
 struct Slab {
   static constexpr bool H = sizeof(T) == 2;
