@@ -332,7 +332,7 @@ int64_t afno_linear_backward_workspace(int64_t M, int64_t K, int64_t N, int dtyp
 }
 
 int64_t afno_layer_norm_backward_workspace(int64_t M, int64_t C, int dtype) {
-  return workspace_of(M, C, C, dtype, [&] {
+  return workspace_of(M, C, 1, dtype, [&] {
     return afno::norm_backward_bytes({nullptr, nullptr, nullptr, nullptr, M, C, 0.f, dtype, nullptr, nullptr, nullptr});
   });
 }

@@ -295,6 +295,11 @@ def check_norm(M, C, residual, dtype, put, mean=0.5):
     close("dbeta", d["dbeta"], dbe, k(M) * U * np.abs(g).sum(0))
 
 
+@pytest.mark.parametrize("dtype", ["fp32", "bf16"])
+def test_layer_norm_of_very_wide_rows(dtype):
+    check_norm(3, 2 ** 17 + 5, True, dtype, store)
+
+
 def test_layer_norm_of_a_large_mean():
     """Rows whose mean is 4,096 times their spread: the squares are taken about the mean."""
     check_norm(50, 512, False, "fp32", store, mean=4096.0)

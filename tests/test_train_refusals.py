@@ -107,6 +107,13 @@ def test_workspace_sizes():
         assert f(9000, 513, 512, BF16, 1) >= 9000 * 520 * 2
 
 
+def test_workspace_sizes_of_the_widest_rows():
+    """What a call takes its workspace query takes: a norm has no array of C x C."""
+    for C in (2 ** 17 + 1, 2 ** 20):
+        assert afno.afno_layer_norm_backward_workspace(3, C, 0) >= 2 * C * 4 + 3 * 8
+    assert afno.afno_layer_norm_backward_workspace(3, 2 ** 20 + 1, 0) == UNS
+
+
 def test_python_refusals():
     torch = pytest.importorskip("torch")
     z = lambda *s, dtype=torch.float32: torch.zeros(*s, dtype=dtype)  # noqa: E731
