@@ -6,7 +6,7 @@
 // One call gives eight 16-bit numbers, which serve the eight elements 8 i .. 8 i + 7 of a tensor's
 // flat index: counter (i low, i high, place low, place high), key the seed.  Sixteen bits rather than
 // thirty-two, so that one call serves the 16 bytes of bf16 that a lane stores at once: its 14 products
-// of 32 x 32 bits are quarter-rate instructions (about 340 issue cycles of a wave a call).
+// of 32 x 32 bits are quarter-rate instructions (about 280 issue cycles of a wave a call).
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>
@@ -21,6 +21,11 @@ struct DropArgs {
   uint32_t threshold;
   float scale;
 };
+
+// a ^ b ^ c in one instruction, which the compiler takes two for
+__device__ __forceinline__ uint32_t xor3(uint32_t a, uint32_t b, uint32_t c) {
+  return __builtin_amdgcn_bitop3_b32(a, b, c, 0x96);
+}
 
 struct Drop {
   uint32_t k0, k1, c2, c3, threshold;
@@ -38,9 +43,9 @@ struct Drop {
 #pragma unroll
     for (int r = 0; r < 7; ++r) {
       const uint64_t p = (uint64_t)x0 * 0xD2511F53u, q = (uint64_t)x2 * 0xCD9E8D57u;
-      x0 = (uint32_t)(q >> 32) ^ x1 ^ a;
+      x0 = xor3((uint32_t)(q >> 32), x1, a);
       x1 = (uint32_t)q;
-      x2 = (uint32_t)(p >> 32) ^ x3 ^ b;
+      x2 = xor3((uint32_t)(p >> 32), x3, b);
       x3 = (uint32_t)p;
       a += 0x9E3779B9u;
       b += 0xBB67AE85u;

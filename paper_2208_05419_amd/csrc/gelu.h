@@ -35,7 +35,7 @@ __device__ __forceinline__ float gelu(float z) {
 // reciprocal and the exponential a last place off (the two terms cancel near z = -0.75, so there is no
 // bound relative to the value).  +inf gives 1, -inf 0, NaN NaN.
 __device__ __forceinline__ float gelu_grad(float z) {
-  const float a = fminf(fabsf(z), 16.f);
+  const float a = __builtin_elementwise_minimum(fabsf(z), 16.f);  // NaN stays
   const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3f, a, 1.f));
   float q = 0.037535712f;
   q = __builtin_fmaf(q, t, -0.16501968f);
@@ -46,11 +46,9 @@ __device__ __forceinline__ float gelu_grad(float z) {
   q = __builtin_fmaf(q, t, 0.1211057f);
   q = __builtin_fmaf(q, t, 0.11960549f);
   const float e = __builtin_amdgcn_exp2f(a * a * -0.72134752f);  // exp(-a^2 / 2)
-  const float u = t * q * e;
-  // a phi(a) - u below zero with its sign turned, 1 - u + a phi(a) above
-  const float d = __builtin_fmaf(a * 0.39894228f, e, -u);
-  const float r = z > 0.f ? 1.f + d : -d;
-  return z != z ? z : r;
+  // a phi(a) - u: below zero with its sign turned, above 1 and this
+  const float d = e * __builtin_fmaf(-t, q, a * 0.39894228f);
+  return z > 0.f ? 1.f + d : -d;
 }
 
 }  // namespace afno
