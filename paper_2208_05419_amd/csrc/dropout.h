@@ -34,8 +34,9 @@ struct Drop {
       : k0((uint32_t)a.seed), k1((uint32_t)(a.seed >> 32)), threshold(a.threshold), scale(a.scale) {
     uint64_t place = a.offset;
     if (a.threshold && a.counter) place += *a.counter;
-    c2 = (uint32_t)place;
-    c3 = (uint32_t)(place >> 32);
+    // the same in every lane: held once a wave
+    c2 = __builtin_amdgcn_readfirstlane((uint32_t)place);
+    c3 = __builtin_amdgcn_readfirstlane((uint32_t)(place >> 32));
   }
   // the eight numbers of group i, two to a word, the lower half first
   __device__ __forceinline__ uint4 numbers(uint64_t i) const {

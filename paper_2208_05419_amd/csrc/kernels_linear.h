@@ -139,8 +139,16 @@ __device__ __forceinline__ void finish_some(const Epilogue<T>& e, const Drop& d,
 }
 template <typename T, int NV>
 __device__ __forceinline__ void load_bias(const Epilogue<T>& e, int64_t N, int64_t n, float (&b)[NV]) {
+  union { uint32_t w[NV * sizeof(T) / 4]; T v[NV]; } u = {};
+  if (e.bias && n + NV <= N) {
+    __builtin_memcpy(u.w, e.bias + n, sizeof(u));  // one load, at any address
+  } else if (e.bias) {
 #pragma unroll
-  for (int j = 0; j < NV; ++j) b[j] = e.bias && n + j < N ? ld_f(e.bias + n + j) : 0.f;
+    for (int j = 0; j < NV; ++j)
+      if (n + j < N) u.v[j] = e.bias[n + j];
+  }
+#pragma unroll
+  for (int j = 0; j < NV; ++j) b[j] = (float)u.v[j];
 }
 
 // Workgroup -> split, tile row and tile column, of 8 ceil(splits tiles / 8) workgroups: workgroup g runs on XCD

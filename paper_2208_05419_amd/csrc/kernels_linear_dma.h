@@ -169,18 +169,19 @@ struct Slab {
 // every 16 and, bf16, columns 8 gq .. + 7 of every 32, fp32, 4 gq .. + 3 of every 16: a store covers 64
 // bytes of 16 rows.  m0, n0: the wave's first row and column.
 template <typename T, bool BR, int TM, int TN>
-__device__ __forceinline__ void dma_store(const GemmArgs<T>& g, const f32x4 (&acc)[TM][TN], int64_t m0,
-                                          int64_t n0, int split, int lane) {
+__device__ __forceinline__ void dma_store(const GemmArgs<T>& g, const Drop& d, const f32x4 (&acc)[TM][TN],
+                                          int64_t m0, int64_t n0, int split, int lane) {
   constexpr int NV = 16 / sizeof(T), PER = NV / 4;
   const int l16 = lane & 15, gq = lane >> 4;
-  const Drop d(g.e.drop);
   const bool units = aligned_units<T, NV>(g.e, g.N);
+  float bias[TN / PER][NV];  // all loads at once
+#pragma unroll
+  for (int h = 0; h < TN / PER; ++h) load_bias(g.e, g.N, n0 + NV * gq + 4 * NV * h, bias[h]);
 #pragma unroll
   for (int h = 0; h < TN / PER; ++h) {
     const int64_t n = n0 + NV * gq + 4 * NV * h;
     if (n >= g.N) continue;
-    float bv[NV];
-    load_bias(g.e, g.N, n, bv);
+    const float(&bv)[NV] = bias[h];
 #pragma unroll
     for (int a = 0; a < TM; ++a) {
       const int64_t m = m0 + 16 * a + l16;
@@ -287,6 +288,9 @@ __global__ void __launch_bounds__(512) gemm_tile256(GemmArgs<bf16> g) {
   if (S) {
     sa.issue(st0 + 64 * wave, 0, g.lda);
     sb.issue(st0 + SA::U + 64 * wave, 0, g.ldb);
+  }
+  const Drop d(g.e.drop);  // its load of the counter under cover of the first stage's
+  if (S) {
     sync();
     if (wave >= 4) dma_barrier();
     int s = 0;
@@ -311,7 +315,7 @@ __global__ void __launch_bounds__(512) gemm_tile256(GemmArgs<bf16> g) {
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(wait_loads(0));
   asm volatile("" ::: "memory");
-  dma_store<bf16, BR, 8, 4>(g, acc, m0 + 128 * wm, n0 + 64 * wn, t.split, lane);
+  dma_store<bf16, BR, 8, 4>(g, d, acc, m0 + 128 * wm, n0 + 64 * wn, t.split, lane);
 }
 
 // Workgroup tile TILE x TILE (128 or 64), 4 waves as 2 x 2, fp32 8 as 2 x 4 (two to a SIMD cover each other's
@@ -382,6 +386,13 @@ __global__ void __launch_bounds__((TileWaves<T>::NT)) gemm_tile(GemmArgs<T> g) {
   };
   if (S) {
     issue(st0, 0);
+    if constexpr (NS == 4) {
+      issue(st1, 1);
+      issue(st2, 2);
+    }
+  }
+  const Drop d(g.e.drop);
+  if (S) {
     int s = 0;
     if constexpr (NS == 2) {
       for (; s + 1 < S; s += 2) {
@@ -395,8 +406,6 @@ __global__ void __launch_bounds__((TileWaves<T>::NT)) gemm_tile(GemmArgs<T> g) {
       sync_all();
       if (S & 1) compute(st0);
     } else {
-      issue(st1, 1);
-      issue(st2, 2);
       for (; s + 3 < S; s += 4) {
         sync();
         issue(st3, s + 3);
@@ -426,7 +435,7 @@ __global__ void __launch_bounds__((TileWaves<T>::NT)) gemm_tile(GemmArgs<T> g) {
     sync_all();
     compute(rest);
   }
-  dma_store<T, BR, TM, TN>(g, acc, m0 + WR * wm, n0 + WC * wn, t.split, lane);
+  dma_store<T, BR, TM, TN>(g, d, acc, m0 + WR * wm, n0 + WC * wn, t.split, lane);
 }
 
 }  // namespace afno
