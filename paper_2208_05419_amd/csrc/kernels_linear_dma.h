@@ -231,9 +231,8 @@ __device__ __forceinline__ void dma_store(const GemmArgs<T>& g, const Drop& d, c
 // The 32 x 32 x 16 instruction, whose lanes hold 32 bytes of 32 rows to store: 565 us and 730 us where
 // this then took 507 and 567 (64,800 x 4,096 x 1,024 and the other way round).
 // Now 446 us = 1.22 PFLOP/s and 545 = 1.00, bound by the matrix cores at the clock that their power leaves and,
-// in the wide product, by an epilogue during which one workgroup a CU leaves them idle: 621 with GELU, 588
-// with dropout, 674 with both, 728 with the value before them stored too, and that 800 where x is not in
-// the caches from the call before (one stage's loads ahead do not cover the memory's latency).
+// in the wide product, by an epilogue during which one workgroup a CU leaves them idle: GELU and dropout, with the
+// value before them stored too, come to about 715.
 template <bool AR, bool BR>
 __global__ void __launch_bounds__(512) gemm_tile256(GemmArgs<bf16> g) {
   typedef Slab<bf16, AR, false, 256, 128, 512> SA;
