@@ -155,9 +155,11 @@ __device__ __forceinline__ void load_bias(const Epilogue<T>& e, int64_t N, int64
 // g % 8, and the workgroups of one XCD take neighbouring ones, column tiles first, then rows, then splits, so
 // that a row tile's operand stays in that XCD's L2 and no XCD has more than its eighth (252 workgroups dealt by
 // tile alone left one XCD with 7 and the others with 35 for 32 CUs: 192 us where 108).  Of eight
-// column tiles or more, rows in groups of eight, a group's columns one after another: the 32 tiles that an XCD has
-// under way then read four column tiles' operand and not all of it, which the L2 does not hold (64,800 x
-// 1,024 x 4,096 with GELU and dropout, x not in the caches: 795 us by rows, 740 by groups of four, 715 of eight).
+// column tiles or more, and of four rounds of the chip or more, rows in groups of eight, a group's columns one
+// after another: the 32 tiles that an XCD has under way then read four column tiles' operand and not all of it, which
+// the L2 does not hold (64,800 x 1,024 x 4,096 with GELU and dropout, 4,064 tiles, x not in the caches: 795 us by
+// rows, 740 by groups of four, 715 of eight; but 4,096 x 1,024 x 4,096, 256 tiles: 35.6 by rows, 37.5 by eight, and
+// 2,001 x 1,001 x 999, 512 tiles: 20.6 and 21.9).
 struct TilePlace {
   int64_t m, n;
   int split;
@@ -169,7 +171,7 @@ struct TilePlace {
     any = (g >> 3) < per && t < all;
     const uint32_t s = t / tiles, i = t - s * tiles, r = i / nc;
     split = (int)s;
-    const uint32_t h0 = nc >= 8 ? 8 : 1, first = r / h0 * h0, in = i - first * nc, h = min(h0, (uint32_t)rows - first);
+    const uint32_t h0 = nc >= 8 && all >= 1024 ? 8 : 1, first = r / h0 * h0, in = i - first * nc, h = min(h0, (uint32_t)rows - first);
     n = in / h;
     m = first + (in - in / h * h);
   }
