@@ -275,7 +275,8 @@ int64_t afno_linear_forward_workspace(int64_t M, int64_t K, int64_t N, int dtype
 /*
  * afno_linear_backward -- gradients of afno_linear_forward for g = dL/dout (the residual's is g):
  *   dz = act'(pre) drop(g);  dx = dz w^T [M][K],  dw = x^T dz [K][N],  db = sum of dz's rows [N]
- * (relu'(0) = 0).  dx, dw and db are in dtype and overwritten; each may be NULL, at least one is not.
+ * With ReLU, dz = drop(g) where pre > 0 and 0 elsewhere (where pre is NaN too), whatever g is there.
+ * dx, dw and db are in dtype and overwritten; each may be NULL, at least one is not.
  * pre is not read where the activation is none, w only for dx, x only for dw.  dz is rounded to dtype
  * before the products; db sums the unrounded values.  M == 0: dw and db are 0.
  */

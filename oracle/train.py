@@ -76,7 +76,11 @@ def linear(x, w, b=None, activation="none", residual=None, **rng):
 
 def linear_backward(g, x, w, pre=None, activation="none", **rng):
     """dx, dw, db and dz."""
-    dz = drop(g, **rng) * (1.0 if activation == "none" else act_slope(pre, activation))
+    dz = drop(g, **rng)
+    if activation == "relu":  # a unit that is off passes on 0, whatever reaches it
+        dz = np.where(pre > 0, dz, 0.0)
+    elif activation != "none":
+        dz = dz * act_slope(pre, activation)
     return dz @ w.T, x.T @ dz, dz.sum(0), dz
 
 

@@ -522,9 +522,9 @@ __global__ void __launch_bounds__(256) dz_kernel(const T* __restrict__ g, const 
       if (act == kActGelu) {
 #pragma unroll
         for (int j = 0; j < 8; ++j) v[j] *= gelu_grad((float)pv.e[j]);
-      } else if (act == kActRelu) {
+      } else if (act == kActRelu) {  // selected: an infinity at a unit that is off is no NaN
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= (float)pv.e[j] > 0.f ? 1.f : 0.f;
+        for (int j = 0; j < 8; ++j) v[j] = (float)pv.e[j] > 0.f ? v[j] : 0.f;
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {
