@@ -8,6 +8,7 @@
 
 #include "kernels_linear_dma.h"
 #include "kernels_norm.h"
+#include "linear_rules.h"
 #include "train_internal.h"
 
 namespace afno {
@@ -22,8 +23,6 @@ auto by_flag(bool v, F f) {
   return v ? f(std::true_type()) : f(std::false_type());
 }
 bool at16(const void* p) { return ((uintptr_t)p & 15) == 0; }  // null counts as aligned
-size_t up256(size_t v) { return (v + 255) / 256 * 256; }
-int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
 // bytes (a multiple of 2, as the address) set to 0: a kernel, so that it replays in a graph
 __global__ void zero_kernel(uint16_t* p, size_t n) {
@@ -36,73 +35,19 @@ void fill_zero(void* p, size_t bytes, hipStream_t st) {
 
 // ---------------------------------------------------------------- products
 
-// How a product is cut: the kernel's square tile, and splits of k whose sums join_splits adds.
-struct Cut {
-  int tile;  // 256: gemm_tile256; 128 or 64: gemm_tile, or gemm_reg where the operands are no 16-byte units
-  int splits;
-  int64_t kper;
-};
-
-// units: the operands are what the direct-to-LDS kernels take.
-// bf16: 256 where most CUs get a tile of it, also by a split of k that leaves 2,048 to each (64,800 k's, 1,024
-// x 4,096: 520 us in four splits of 256 against 693 in two of 128; 1,080 x 1,536 x 768, 30 tiles: 20 against
-// 8 with 64).  Both: 128 where every CU gets one (bf16, 4,096 x 1,024 x 1,024, 256 tiles: 16.5 us, 64
-// 16.6; 10,368 x 1,536 x 384, 972 tiles: 22 and 32; fp32 from three in four: 10,368 x 384 x 1,536, 243
-// tiles: 116 and 122), or by splits of long sums (bf16, 10,368 k's in 384 x 1,536: 35 us in eight of 128, 41
-// with 64 whole), in fp32 two to a CU where 2,048 k's are left to each (20,000 k's, 2,048 x 2,048: 1,291 us
-// in two splits, 1,549 whole; but 10,368 k's in 384 x 1,536: 123 in seven, 152 in ten).
-// Else 64, split where the tiles leave CUs without one and the sum is long: a split costs the join's launch,
-// about 3 us, and a stage of k's 0.2 us, in fp32 0.7 (bf16, 256 x 1,024 x 4,096, 64 tiles: 16.6 us whole,
-// 13.0 in four; 64 x 4,096 x 1,024: 6.3 whole, 8.7 in two; fp32 23.7 whole, 12.9 in four).
-// Without units every k-stage waits for its loads: splits until there are two workgroups a CU.
-Cut cut_product(int64_t M, int64_t N, int64_t K, int es, bool units) {
-  Cut c;
-  auto tiles = [&](int t) { return ceil_div(M, t) * ceil_div(N, t); };
-  auto cut = [&](int tile, int64_t s) {
-    const int stage = 128 / es;
-    c.tile = tile;
-    c.kper = std::max<int64_t>(stage, ceil_div(ceil_div(K, s), stage) * stage);
-    c.splits = (int)ceil_div(K, c.kper);
-    return c;
-  };
-  auto fill = [&](int64_t t, int64_t want, int64_t least) {  // splits for `want` workgroups
-    return std::max<int64_t>(1, std::min<int64_t>(want / t, K / least));
-  };
-  if (!units) {
-    const int tile = M > 64 && N > 64 && tiles(128) * std::max<int64_t>(1, K / 256) >= 256 ? 128 : 64;
-    return cut(tile, tiles(tile) >= 256 ? 1 : fill(tiles(tile), 512, tile == 128 ? 256 : 128));
-  }
-  if (es == 2) {
-    const int64_t s = tiles(256) >= 128 ? 1 : fill(tiles(256), 256, 2048);
-    if (tiles(256) * s >= 128) return cut(256, s);
-  }
-  const int64_t t128 = tiles(128);
-  if (K >= 8192 && M > 64 && N > 64 && t128 < 512) {
-    const bool two = es == 4 && 512 / t128 >= 1 && K / (512 / t128) >= 2048;
-    return cut(128, fill(t128, two ? 512 : 256, 1024));
-  }
-  if (t128 >= 256 || (es == 4 && t128 >= 192)) return cut(128, 1);
-  return cut(64, tiles(64) >= 256 ? 1 : fill(tiles(64), 256, es == 2 ? 1024 : 256));
-}
-size_t part_of(int64_t M, int64_t N, const Cut& c) {
-  return c.splits > 1 ? (size_t)c.splits * M * N * sizeof(float) : 0;
-}
-// Whether linear_rows takes a forward product.  bf16, 1,024 x 4,096: 3.9 us for one row, 4.5 for two, 6.0 for
-// four, where gemm_tile takes 6.5 for any; fp32 5.2 for eight, 9 for sixteen against 12.
-bool few_rows(int64_t M, int es) { return M <= (es == 2 ? 2 : 16); }
-// whatever the addresses turn out to be
-size_t part_bytes(int64_t M, int64_t N, int64_t K, int dtype) {
-  const int es = dtype == 0 ? 4 : 2;
-  return std::max(part_of(M, N, cut_product(M, N, K, es, false)), part_of(M, N, cut_product(M, N, K, es, true)));
-}
-
-// One product with its epilogue; part: room for part_bytes.  Operands at any address and stride: the
-// direct-to-LDS kernels where both are 16-byte units, else gemm_reg.
+// One product with its epilogue, a and b given, the rest of it by p; part: room for part_bytes.
 template <typename T, bool AR, bool BR>
-hipError_t product(GemmArgs<T> g, float* part, hipStream_t st) {
-  constexpr int UE = Unit<T>::UE;
+hipError_t product(GemmArgs<T> g, const Product& p, float* part, hipStream_t st) {
+  g.lda = p.lda;
+  g.ldb = p.ldb;
+  g.M = p.M;
+  g.N = p.N;
+  g.K = p.K;
+  g.ma = p.ma;
+  g.nb = p.nb;
+  const Path path = product_path(p, (int)sizeof(T));
   if constexpr (!AR && BR) {
-    if (few_rows(g.M, (int)sizeof(T))) {
+    if (path.rows) {
       const int mr = g.M >= 3 ? 4 : (int)g.M;
       const dim3 grid((unsigned)ceil_div(g.N, kRowsCols), (unsigned)ceil_div(g.M, mr));
       if (mr == 1) hipLaunchKernelGGL((linear_rows<T, 1>), grid, dim3(1024), 0, st, g);
@@ -111,16 +56,14 @@ hipError_t product(GemmArgs<T> g, float* part, hipStream_t st) {
       return hipGetLastError();
     }
   }
-  const bool units = g.lda % UE == 0 && g.ldb % UE == 0 && at16(g.a) && at16(g.b) &&
-                     (!AR || g.ma % UE == 0) && (!BR || g.nb % UE == 0);
-  const Cut c = cut_product(g.M, g.N, g.K, (int)sizeof(T), units);
+  const Cut& c = path.cut;
   const dim3 grid((unsigned)(8 * ceil_div(c.splits * ceil_div(g.M, c.tile) * ceil_div(g.N, c.tile), 8)));
   g.splits = c.splits;
   g.kper = c.kper;
   g.part = c.splits > 1 ? part : nullptr;
   if (c.tile == 256) {
     if constexpr (sizeof(T) == 2) hipLaunchKernelGGL((gemm_tile256<AR, BR>), grid, dim3(512), 0, st, g);
-  } else if (units) {
+  } else if (path.units) {
     if (c.tile == 128) hipLaunchKernelGGL((gemm_tile<T, AR, BR, 128>), grid, dim3(TileWaves<T>::NT), 0, st, g);
     else hipLaunchKernelGGL((gemm_tile<T, AR, BR, 64>), grid, dim3(TileWaves<T>::NT), 0, st, g);
   } else {
@@ -133,16 +76,6 @@ hipError_t product(GemmArgs<T> g, float* part, hipStream_t st) {
   return hipGetLastError();
 }
 
-// Whether operands that are no 16-byte units are copied to rows that are, for the direct-to-LDS kernels: a
-// launch and a pass over them, against loads through registers.  bf16: 2,001 x 1,001 x 999 20 us, not
-// copied 46; 300 x 77 x 333 7.6 and 6.3, but its gradients, whose factor dz comes in such rows anyway, 20 and 26.
-// fp32, whose matrix instructions take longer than the loads: 54 and 74, but 1,000 x 1,001 x 501 27 and
-// 27, and 64,800 x 77 x 1,023 with few operations to a byte 242 and 215.
-bool worth_packing(int64_t M, int64_t K, int64_t N, int es, bool backward) {
-  const double work = (double)M * (double)K * (double)N;
-  if (es == 2) return work >= (backward ? 1 << 22 : 1 << 26);
-  return work >= 1 << 30 && std::min(K, N) >= 256;
-}
 template <typename T>
 void pack(const PackArgs<T>& a, const PackArgs<T>& b, hipStream_t st) {
   constexpr int UE = Unit<T>::UE;
@@ -151,100 +84,42 @@ void pack(const PackArgs<T>& a, const PackArgs<T>& b, hipStream_t st) {
     hipLaunchKernelGGL((pack_rows<T>), dim3((unsigned)std::min<int64_t>(1 << 20, ceil_div(units, 256))), dim3(256),
                        0, st, a, b);
 }
-int64_t whole_units(int64_t n, int es) { return ceil_div(n, 16 / es) * (16 / es); }
 
-// Chunks of rows of the column sums: as many as fill the chip eight times with 256-column workgroups, of at
-// least eight rows, one to a thread (1,080 x 1,536: 11.3 us with 32, 8.1 with eight).
-int64_t chunk_rows(int64_t M, int64_t N) {
-  const int64_t want = std::max<int64_t>(1, 2048 / ceil_div(N, 256));
-  return std::max<int64_t>(8, ceil_div(ceil_div(M, want), 8) * 8);
+LinearSizes sizes_of(const LinearFwd& a) {
+  return {a.M, a.K, a.N, a.dtype == 0 ? 4 : 2, at16(a.x), at16(a.w), true, false, false, false, false};
 }
-
-// A call's workspace: copies of operands that are no 16-byte units (whatever the addresses turn out to be,
-// room for them where the sizes are worth it), the factor dz, chunk sums, the splits' sums.
-struct Layout {
-  bool packing, need_dz;
-  int64_t kp, np;  // rows of the copies and of dz
-  size_t x, w, dz, sums, part, bytes;
-};
-Layout forward_layout(const LinearFwd& a) {
-  Layout l = {};
-  const int es = a.dtype == 0 ? 4 : 2;
-  if (few_rows(a.M, es)) return l;
-  l.packing = worth_packing(a.M, a.K, a.N, es, false);
-  l.kp = whole_units(a.K, es);
-  l.np = whole_units(a.N, es);
-  size_t at = 0;
-  l.x = at;
-  if (l.packing && (l.kp != a.K || !at16(a.x))) at += up256((size_t)a.M * l.kp * es);
-  l.w = at;
-  if (l.packing && (l.np != a.N || !at16(a.w))) at += up256((size_t)a.K * l.np * es);
-  l.part = at;
-  l.bytes = at + part_bytes(a.M, a.N, a.K, a.dtype);
-  return l;
-}
-Layout backward_layout(const LinearBwd& a) {
-  Layout l = {};
-  const int es = a.dtype == 0 ? 4 : 2;
-  l.packing = worth_packing(a.M, a.K, a.N, es, true);
-  l.kp = whole_units(a.K, es);
-  l.np = l.packing ? ceil_div(a.N, 8) * 8 : a.N;
-  l.need_dz = (a.dx || a.dw) &&
-              (a.act != kActNone || a.drop.threshold || (l.packing && (l.np != a.N || !at16(a.g))));
-  if (l.need_dz) l.np = ceil_div(a.N, 8) * 8;
-  size_t at = 0;
-  l.x = at;
-  if (l.packing && a.dw && (l.kp != a.K || !at16(a.x))) at += up256((size_t)a.M * l.kp * es);
-  l.w = at;
-  if (l.packing && a.dx && (l.np != a.N || !at16(a.w))) at += up256((size_t)a.K * l.np * es);
-  l.dz = at;
-  if (l.need_dz) at += up256((size_t)a.M * l.np * es);
-  l.sums = at;
-  if (a.db) at += up256((size_t)ceil_div(a.M, chunk_rows(a.M, a.N)) * a.N * sizeof(float));
-  l.part = at;
-  size_t p = 0;
-  if (a.dx) p = part_bytes(a.M, a.K, a.N, a.dtype);
-  if (a.dw) p = std::max(p, part_bytes(a.K, a.N, a.M, a.dtype));
-  l.bytes = at + p;
-  return l;
+LinearSizes sizes_of(const LinearBwd& a) {
+  return {a.M, a.K, a.N, a.dtype == 0 ? 4 : 2, at16(a.x), at16(a.w), at16(a.g), a.dx != nullptr, a.dw != nullptr, a.db != nullptr,
+          a.act != kActNone || a.drop.threshold != 0};
 }
 
 }  // namespace
 
-size_t linear_forward_bytes(const LinearFwd& a) { return forward_layout(a).bytes; }
+size_t linear_forward_bytes(const LinearFwd& a) { return forward_layout(sizes_of(a)).bytes; }
 
 hipError_t launch_linear_forward(const LinearFwd& a, void* ws, hipStream_t st) {
-  const Layout l = forward_layout(a);
+  const LinearSizes sizes = sizes_of(a);
+  const Layout l = forward_layout(sizes);
   char* base = static_cast<char*>(ws);
   return by_type(a.dtype, [&](auto z) {
     typedef decltype(z) T;
     GemmArgs<T> g = {};
     g.a = static_cast<const T*>(a.x);
     g.b = static_cast<const T*>(a.w);
-    g.lda = a.K;
-    g.ldb = a.N;
-    g.M = g.ma = a.M;
-    g.N = g.nb = a.N;
-    g.K = a.K;
     g.e = {static_cast<const T*>(a.b), static_cast<const T*>(a.residual), static_cast<T*>(a.out),
            static_cast<T*>(a.pre), a.act, a.drop};
     PackArgs<T> px = {}, pw = {};
-    if (l.w != l.x) px = {g.a, reinterpret_cast<T*>(base + l.x), a.M, a.K, l.kp};
-    if (l.part != l.w) pw = {g.b, reinterpret_cast<T*>(base + l.w), a.K, a.N, l.np};
+    if (l.copy_x) px = {g.a, reinterpret_cast<T*>(base + l.x), a.M, a.K, l.kp};
+    if (l.copy_w) pw = {g.b, reinterpret_cast<T*>(base + l.w), a.K, a.N, l.np};
     pack(px, pw, st);
-    if (px.rows) {
-      g.a = px.dst;
-      g.lda = l.kp;
-    }
-    if (pw.rows) {
-      g.b = pw.dst;
-      g.ldb = g.nb = l.np;
-    }
-    return product<T, false, true>(g, l.bytes > l.part ? reinterpret_cast<float*>(base + l.part) : nullptr, st);
+    if (l.copy_x) g.a = px.dst;
+    if (l.copy_w) g.b = pw.dst;
+    return product<T, false, true>(g, forward_product(sizes, l),
+                                   l.bytes > l.part ? reinterpret_cast<float*>(base + l.part) : nullptr, st);
   });
 }
 
-size_t linear_backward_bytes(const LinearBwd& a) { return backward_layout(a).bytes; }
+size_t linear_backward_bytes(const LinearBwd& a) { return backward_layout(sizes_of(a)).bytes; }
 
 hipError_t launch_linear_backward(const LinearBwd& a, void* ws, hipStream_t st) {
   if (a.M == 0) {  // sums over no row
@@ -253,7 +128,8 @@ hipError_t launch_linear_backward(const LinearBwd& a, void* ws, hipStream_t st) 
     if (a.db) fill_zero(a.db, (size_t)a.N * es, st);
     return hipGetLastError();
   }
-  const Layout l = backward_layout(a);
+  const LinearSizes sizes = sizes_of(a);
+  const Layout l = backward_layout(sizes);
   char* base = static_cast<char*>(ws);
   return by_type(a.dtype, [&](auto z) -> hipError_t {
     typedef decltype(z) T;
@@ -263,8 +139,8 @@ hipError_t launch_linear_backward(const LinearBwd& a, void* ws, hipStream_t st) 
     float* sums = reinterpret_cast<float*>(base + l.sums);
     float* part = reinterpret_cast<float*>(base + l.part);
     PackArgs<T> px = {}, pw = {};
-    if (l.w != l.x) px = {x, reinterpret_cast<T*>(base + l.x), a.M, a.K, l.kp};
-    if (l.dz != l.w) pw = {w, reinterpret_cast<T*>(base + l.w), a.K, a.N, l.np};
+    if (l.copy_x) px = {x, reinterpret_cast<T*>(base + l.x), a.M, a.K, l.kp};
+    if (l.copy_w) pw = {w, reinterpret_cast<T*>(base + l.w), a.K, a.N, l.np};
     pack(px, pw, st);
     if (l.need_dz || a.db) {
       const int64_t rows = chunk_rows(a.M, a.N), chunks = ceil_div(a.M, rows);
@@ -280,31 +156,20 @@ hipError_t launch_linear_backward(const LinearBwd& a, void* ws, hipStream_t st) 
       if (e != hipSuccess) return e;
     }
     const T* dz = l.need_dz ? dzw : g;
-    const int64_t ldz = l.need_dz ? l.np : a.N;
     if (a.dx) {
       GemmArgs<T> p = {};
       p.a = dz;
-      p.lda = ldz;
-      p.b = pw.rows ? pw.dst : w;
-      p.ldb = pw.rows ? l.np : a.N;
-      p.M = p.ma = a.M;
-      p.N = p.nb = a.K;
-      p.K = a.N;
+      p.b = l.copy_w ? pw.dst : w;
       p.e.out = static_cast<T*>(a.dx);
-      const hipError_t e = product<T, false, false>(p, part, st);
+      const hipError_t e = product<T, false, false>(p, dx_product(sizes, l), part, st);
       if (e != hipSuccess) return e;
     }
     if (a.dw) {
       GemmArgs<T> p = {};
-      p.a = px.rows ? px.dst : x;
-      p.lda = p.ma = px.rows ? l.kp : a.K;
+      p.a = l.copy_x ? px.dst : x;
       p.b = dz;
-      p.ldb = p.nb = ldz;
-      p.M = a.K;
-      p.N = a.N;
-      p.K = a.M;
       p.e.out = static_cast<T*>(a.dw);
-      const hipError_t e = product<T, true, true>(p, part, st);
+      const hipError_t e = product<T, true, true>(p, dw_product(sizes, l), part, st);
       if (e != hipSuccess) return e;
     }
     return hipSuccess;
