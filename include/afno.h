@@ -73,7 +73,12 @@ enum {
  * 32 MB come, outside stream capture, from at most 8 pieces of 32 MB of that pool which the
  * library keeps per device; a stream takes over a piece of another one only when that one's work
  * in it has ended, and each user is ordered behind the last by an event.  Pieces no call is
- * using are given back when a workspace would not fit otherwise.
+ * using are given back when a workspace would not fit otherwise.  Under stream capture the workspace
+ * is memory that the graph allocates and frees by itself, and a graph takes one call that does so, of all entry
+ * points that allocate (this one, _hidden, _stage, _backward, afno_block_forward): the next one in the same
+ * capture returns AFNO_ERR_UNSUPPORTED with nothing recorded, since a replay of several has
+ * read memory that was not there any more.  A captured step takes afno_filter_forward_noalloc, any
+ * number of times.
  * The call is asynchronous: it enqueues on `stream` and returns.
  * B == 0 returns AFNO_OK without touching the GPU (x and out may then be NULL).
  * Errors: arguments are validated before any HIP call; on a non-OK return nothing

@@ -239,6 +239,42 @@ hipEvent_t* profile_slot() {
   return &g_prof.ev[afno::kProfEvents * (size_t)g_prof.used++];
 }
 
+// The workspace of a call.  Under capture it is memory that the graph allocates and frees by itself, and a graph
+// gets one such piece: with one in each of several calls of a graph, a kernel of a replay has read its piece
+// when it was not there any more (a GPU fault; each call alone in its graph was right), and the reason
+// has not been found.  The captures are told apart by their ids, of which the last 64 are kept.
+int acquire(afno::Workspace& ws, size_t bytes, hipStream_t stream) {
+  static std::mutex mu;
+  static unsigned long long taken[64];
+  static int next = 0, count = 0;
+  hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
+  unsigned long long id = 0;
+  hipError_t e = hipStreamGetCaptureInfo(stream, &cap, &id);
+  if (e != hipSuccess) {
+    (void)hipGetLastError();
+    return fail(AFNO_ERR_HIP, std::string("hipStreamGetCaptureInfo: ") + hipGetErrorString(e));
+  }
+  std::unique_lock<std::mutex> lk(mu, std::defer_lock);
+  if (cap != hipStreamCaptureStatusNone) {
+    lk.lock();
+    if (std::find(taken, taken + count, id) != taken + count)
+      return fail(AFNO_ERR_UNSUPPORTED, "a graph takes one call that allocates its workspace: record the others with "
+                                        "afno_filter_forward_noalloc or into graphs of their own");
+  }
+  e = ws.acquire(bytes, stream);
+  if (e != hipSuccess) {
+    (void)hipGetLastError();
+    return fail(AFNO_ERR_HIP, std::string("workspace allocation of ") + std::to_string(bytes) +
+                                  " bytes: " + hipGetErrorString(e));
+  }
+  if (lk.owns_lock()) {
+    taken[next] = id;
+    next = (next + 1) % 64;
+    count = std::min(count + 1, 64);
+  }
+  return AFNO_OK;
+}
+
 // noalloc: the workspace is the current device's scratch array (no allocation); a plan
 // whose workspace exceeds it is rejected before any HIP call.
 int run(const Args& a, int stage, float* dst, hipStream_t stream, bool noalloc = false) {
@@ -285,13 +321,9 @@ int run(const Args& a, int stage, float* dst, hipStream_t stream, bool noalloc =
     return AFNO_OK;
   }
   afno::Workspace ws;
-  e = ws.acquire(pl.ws_bytes, stream);
+  rc = acquire(ws, pl.ws_bytes, stream);
+  if (rc != AFNO_OK) return rc;
   S = ws.ptr;
-  if (e != hipSuccess) {
-    (void)hipGetLastError();
-    return fail(AFNO_ERR_HIP, std::string("workspace allocation of ") +
-                                  std::to_string(pl.ws_bytes) + " bytes: " + hipGetErrorString(e));
-  }
   hipEvent_t* ev = stage == afno::kStageFull ? profile_slot() : nullptr;
   e = afno::launch_filter(pl, a.x, a.w1, a.b1, a.w2, a.b2, S, a.out, dst, stage, stream, ev);
   hipError_t ef = ws.release();
@@ -357,12 +389,8 @@ int run_backward(const Args& a, const void* gout, float* dw1, float* db1, float*
   pl.bwd.acc_offset = pl.bwd.modes_offset + up(modes_bytes);
   pl.bwd.bytes = pl.bwd.acc_offset + afno::bwd_acc_floats(pl) * 4;
   afno::Workspace ws;
-  e = ws.acquire(pl.bwd.bytes, stream);
-  if (e != hipSuccess) {
-    (void)hipGetLastError();
-    return fail(AFNO_ERR_HIP, std::string("workspace allocation of ") + std::to_string(pl.bwd.bytes) +
-                                  " bytes: " + hipGetErrorString(e));
-  }
+  rc = acquire(ws, pl.bwd.bytes, stream);
+  if (rc != AFNO_OK) return rc;
   bp.ws = ws.ptr;
   e = afno::launch_backward(pl, bp, stream);
   hipError_t ef = ws.release();
@@ -419,14 +447,10 @@ int run_block(const Args& a, const void* ln1_g, const void* ln1_b, const void* l
   bp.s_off = bp.wbt_off + up(mb);
   const size_t bytes = bp.s_off + pl.ws_bytes;
   afno::Workspace ws;
-  hipError_t e = ws.acquire(bytes, stream);
-  if (e != hipSuccess) {
-    (void)hipGetLastError();
-    return fail(AFNO_ERR_HIP, std::string("workspace allocation of ") + std::to_string(bytes) +
-                                  " bytes: " + hipGetErrorString(e));
-  }
+  rc = acquire(ws, bytes, stream);
+  if (rc != AFNO_OK) return rc;
   bp.ws = static_cast<char*>(ws.ptr);
-  e = afno::launch_block(pl, bp, stream);
+  hipError_t e = afno::launch_block(pl, bp, stream);
   hipError_t ef = ws.release();
   if (e != hipSuccess) return fail(AFNO_ERR_HIP, std::string("launch: ") + hipGetErrorString(e));
   if (ef != hipSuccess) return fail(AFNO_ERR_HIP, std::string("workspace free: ") + hipGetErrorString(ef));

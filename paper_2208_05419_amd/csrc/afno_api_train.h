@@ -78,8 +78,7 @@ int check_workspace(const void* ws, int64_t have, size_t need, std::initializer_
 }
 
 // The launch with its workspace (bytes == 0: none): the caller's, else one of the library's.  Those
-// are not for a captured call: memory that a graph allocates and frees by itself, several times in a
-// graph, was not there for its last reader in a replay.
+// are not for a captured call: a step has many of these, and a graph takes one call that allocates (acquire()).
 template <typename F>
 int with_workspace(void* given, size_t bytes, hipStream_t stream, F launch) {
   if (given || !bytes) {
@@ -95,14 +94,8 @@ int with_workspace(void* given, size_t bytes, hipStream_t stream, F launch) {
   if (cap != hipStreamCaptureStatusNone)
     return fail(AFNO_ERR_UNSUPPORTED, "a captured call needs a workspace of the caller's");
   afno::Workspace ws;
-  {
-    e = ws.acquire(bytes, stream);
-    if (e != hipSuccess) {
-      (void)hipGetLastError();
-      return fail(AFNO_ERR_HIP, std::string("workspace allocation of ") + std::to_string(bytes) +
-                                    " bytes: " + hipGetErrorString(e));
-    }
-  }
+  const int rc = acquire(ws, bytes, stream);
+  if (rc != AFNO_OK) return rc;
   e = launch(ws.ptr);
   ef = ws.release();
   if (e != hipSuccess) return fail(AFNO_ERR_HIP, std::string("launch: ") + hipGetErrorString(e));
