@@ -13,6 +13,7 @@
 
 #include "afno.h"
 #include "afno_internal.h"
+#include "train_internal.h"
 #include "workspace.h"
 
 namespace {
@@ -305,7 +306,8 @@ int run(const Args& a, int stage, float* dst, hipStream_t stream, bool noalloc =
     else {
       const size_t n = stage == afno::kStageDelta ? (size_t)a.B * a.H * a.W * a.C
                                                   : (size_t)a.B * a.H * (a.W / 2 + 1) * a.C * 2;
-      e = hipMemsetAsync(dst, 0, n * sizeof(float), stream);
+      afno::fill_zero(dst, n * sizeof(float), stream);
+      e = hipGetLastError();
     }
     if (e != hipSuccess) return fail(AFNO_ERR_HIP, std::string("copy: ") + hipGetErrorString(e));
     return AFNO_OK;

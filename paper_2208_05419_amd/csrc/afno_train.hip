@@ -24,13 +24,8 @@ auto by_flag(bool v, F f) {
 }
 bool at16(const void* p) { return ((uintptr_t)p & 15) == 0; }  // null counts as aligned
 
-// bytes (a multiple of 2, as the address) set to 0: a kernel, so that it replays in a graph
 __global__ void zero_kernel(uint16_t* p, size_t n) {
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) p[i] = 0;
-}
-void fill_zero(void* p, size_t bytes, hipStream_t st) {
-  hipLaunchKernelGGL(zero_kernel, dim3((unsigned)std::min<size_t>(1024, (bytes / 2 + 255) / 256)), dim3(256),
-                     0, st, static_cast<uint16_t*>(p), bytes / 2);
 }
 
 // ---------------------------------------------------------------- products
@@ -94,6 +89,11 @@ LinearSizes sizes_of(const LinearBwd& a) {
 }
 
 }  // namespace
+
+void fill_zero(void* p, size_t bytes, hipStream_t st) {
+  hipLaunchKernelGGL(zero_kernel, dim3((unsigned)std::min<size_t>(1024, (bytes / 2 + 255) / 256)), dim3(256),
+                     0, st, static_cast<uint16_t*>(p), bytes / 2);
+}
 
 size_t linear_forward_bytes(const LinearFwd& a) { return forward_layout(sizes_of(a)).bytes; }
 

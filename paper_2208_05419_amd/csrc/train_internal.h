@@ -48,6 +48,9 @@ struct DropRunArgs {
   void* out;
 };
 
+// bytes > 0 (a multiple of 2, as the address) set to 0: a kernel, since a graph's memset nodes have not
+// replayed reliably
+void fill_zero(void* p, size_t bytes, hipStream_t st);
 // workspace bytes (0: none), and the launches with that much at ws
 size_t linear_forward_bytes(const LinearFwd& a);
 hipError_t launch_linear_forward(const LinearFwd& a, void* ws, hipStream_t st);

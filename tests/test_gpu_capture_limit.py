@@ -119,3 +119,22 @@ def test_a_captured_step_without_allocations(data):
         assert all(torch.equal(a, b) for a, b in zip(held, want))
         step()
         torch.cuda.synchronize()
+
+
+@pytest.mark.parametrize("stage", [afno.AFNO_STAGE_SPECTRUM, afno.AFNO_STAGE_MIXED, afno.AFNO_STAGE_DELTA])
+def test_a_captured_stage_of_nothing_kept(data, stage):
+    """No mode passes: the stage is 0, in every replay whatever its memory held before."""
+    x, args, _ = data
+    call = lambda: afno.filter_stage(x, *args, 0.01, stage)  # noqa: E731
+    want = call()
+    torch.cuda.synchronize()
+    assert not want.any()
+    with _capture() as graph:
+        held = call()
+    for rep in range(4):
+        held.fill_(float(rep + 1))
+        torch.cuda.synchronize()
+        graph.replay()
+        call()
+        torch.cuda.synchronize()
+        assert not held.any()
