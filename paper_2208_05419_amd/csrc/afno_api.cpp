@@ -250,10 +250,9 @@ int acquire(afno::Workspace& ws, size_t bytes, hipStream_t stream) {
   static int next = 0, count = 0;
   hipStreamCaptureStatus cap = hipStreamCaptureStatusNone;
   unsigned long long id = 0;
-  hipError_t e = hipStreamGetCaptureInfo(stream, &cap, &id);
-  if (e != hipSuccess) {
+  if (hipStreamGetCaptureInfo(stream, &cap, &id) != hipSuccess) {  // the null stream beside another's capture
     (void)hipGetLastError();
-    return fail(AFNO_ERR_HIP, std::string("hipStreamGetCaptureInfo: ") + hipGetErrorString(e));
+    cap = hipStreamCaptureStatusNone;
   }
   std::unique_lock<std::mutex> lk(mu, std::defer_lock);
   if (cap != hipStreamCaptureStatusNone) {
@@ -262,7 +261,7 @@ int acquire(afno::Workspace& ws, size_t bytes, hipStream_t stream) {
       return fail(AFNO_ERR_UNSUPPORTED, "a graph takes one call that allocates its workspace: record the others with "
                                         "afno_filter_forward_noalloc or into graphs of their own");
   }
-  e = ws.acquire(bytes, stream);
+  const hipError_t e = ws.acquire(bytes, stream);
   if (e != hipSuccess) {
     (void)hipGetLastError();
     return fail(AFNO_ERR_HIP, std::string("workspace allocation of ") + std::to_string(bytes) +
