@@ -242,14 +242,14 @@ int afno_filter_backward(const void* x, const void* w1, const void* b1, const vo
  * contiguous device memory on the current device, aligned to their element (16 bytes take the wider
  * kernels).  Any M from 0 to 2^25, any width up to 2^20, up to 2^34 values an array
  * (AFNO_ERR_UNSUPPORTED beyond).  No output may overlap an input or another output
- * (AFNO_ERR_ALIAS).  Ownership, asynchrony and errors as afno_filter_forward; sums are held in float32 and added in a fixed order, so repeated calls give
- * the same bits.
+ * (AFNO_ERR_ALIAS).  Ownership, asynchrony and errors as afno_filter_forward; sums are held in float32
+ * and added in a fixed order, so repeated calls give the same bits.
  *
  * Workspace.  afno_*_workspace gives the bytes that a call of these sizes may need (0: none; an error
  * code for sizes that the call refuses); aligned non-zero: for arrays that are all 16-byte aligned,
  * which may need less (rows at other addresses are copied).  With workspace non-NULL the call uses
- * the caller's memory: at least that many bytes, 16-byte aligned, apart from every array, the call's alone until its work
- * has ended, so that captured graphs that may run at the same time need one each.  With NULL the
+ * the caller's memory: at least that many bytes, 16-byte aligned, apart from every array, the call's
+ * alone until its work has ended, so that captured graphs that may run at the same time need one each.  With NULL the
  * library takes one of its own as afno_filter_forward does, except under stream capture, where a
  * call that needs one returns AFNO_ERR_UNSUPPORTED.
  *
@@ -283,7 +283,8 @@ int64_t afno_linear_forward_workspace(int64_t M, int64_t K, int64_t N, int dtype
  * With ReLU, dz = drop(g) where pre > 0 and 0 elsewhere (where pre is NaN too), whatever g is there.
  * dx, dw and db are in dtype and overwritten; each may be NULL, at least one is not.
  * pre is not read where the activation is none, w only for dx, x only for dw.  dz is rounded to dtype
- * before the products; db sums the unrounded values.  M == 0: dw and db are 0.
+ * before the products; db sums the unrounded values.  dw and db are each rounded once from their float32
+ * sums: a caller that adds up several bf16 batches' adds their roundings.  M == 0: dw and db are 0.
  */
 int afno_linear_backward(const void* g, const void* x, const void* w, const void* pre, int64_t M,
                          int64_t K, int64_t N, int activation, float p, uint64_t seed,

@@ -6,8 +6,8 @@ hand-written HIP kernels behind the C ABI of ``include/afno.h``, and so do the o
 train the rest of an AFNO block (linear products, LayerNorm, dropout); this package is its
 Python binding.  Importing it loads nothing; the library is loaded on first use.
 """
-from .afno import (AFNO_ACT_GELU, AFNO_ACT_NONE, AFNO_ACT_RELU, AFNO_DTYPE_BF16, AFNO_DTYPE_FP32, AFNO_ERR_ALIAS, AFNO_ERR_HIP,  # noqa: F401
-                   AFNO_ERR_INVALID_ARG, AFNO_ERR_UNSUPPORTED, AFNO_OK, AFNO_PATH_AUTO,
+from .afno import (AFNO_ACT_GELU, AFNO_ACT_NONE, AFNO_ACT_RELU,  # noqa: F401
+                   AFNO_DTYPE_BF16, AFNO_DTYPE_FP32, AFNO_ERR_ALIAS, AFNO_ERR_HIP, AFNO_ERR_INVALID_ARG, AFNO_ERR_UNSUPPORTED, AFNO_OK, AFNO_PATH_AUTO,
                    AFNO_PATH_GENERIC, AFNO_PATH_VALU_DFT, AFNO_STAGE_DELTA,
                    AFNO_STAGE_MIXED, AFNO_STAGE_SPECTRUM, EXPORTED, LIB_PATH, AfnoError,
                    BLOCK_PARAMS, KERNELS, afno_block_forward, afno_filter_backward, afno_filter_forward, afno_filter_forward_hidden,
@@ -20,5 +20,5 @@ from .afno import (AFNO_ACT_GELU, AFNO_ACT_NONE, AFNO_ACT_RELU, AFNO_DTYPE_BF16,
 from .train import (ACTIVATIONS, afno_dropout_backward, afno_dropout_forward,  # noqa: F401
                     afno_layer_norm_backward, afno_layer_norm_backward_workspace,
                     afno_layer_norm_forward, afno_linear_backward, afno_linear_backward_workspace,
-                    afno_linear_forward, afno_linear_forward_workspace, dropout_backward, dropout_forward, layer_norm_backward,
-                    layer_norm_forward, linear_backward, linear_forward)
+                    afno_linear_forward, afno_linear_forward_workspace, dropout_backward,
+                    dropout_forward, layer_norm_backward, layer_norm_forward, linear_backward, linear_forward)

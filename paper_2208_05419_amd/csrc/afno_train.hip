@@ -84,8 +84,8 @@ LinearSizes sizes_of(const LinearFwd& a) {
   return {a.M, a.K, a.N, a.dtype == 0 ? 4 : 2, at16(a.x), at16(a.w), true, false, false, false, false};
 }
 LinearSizes sizes_of(const LinearBwd& a) {
-  return {a.M, a.K, a.N, a.dtype == 0 ? 4 : 2, at16(a.x), at16(a.w), at16(a.g), a.dx != nullptr, a.dw != nullptr, a.db != nullptr,
-          a.act != kActNone || a.drop.threshold != 0};
+  return {a.M, a.K, a.N, a.dtype == 0 ? 4 : 2, at16(a.x), at16(a.w), at16(a.g), a.dx != nullptr, a.dw != nullptr,
+          a.db != nullptr, a.act != kActNone || a.drop.threshold != 0};
 }
 
 }  // namespace
@@ -209,8 +209,8 @@ hipError_t launch_norm_forward(const NormFwd& a, hipStream_t st) {
       by_flag(vec, [&](auto v) {
         by_capacity(a.C, [&](auto cap, auto w) {
           hipLaunchKernelGGL((norm_rows<T, decltype(v)::value, decltype(cap)::value, decltype(w)::value>),
-                             dim3((unsigned)ceil_div(a.M, 4 / decltype(w)::value)), dim3(256), 0, st, x, r, ga, be, out, sum, a.M,
-                             (int)a.C, a.eps);
+                             dim3((unsigned)ceil_div(a.M, 4 / decltype(w)::value)), dim3(256), 0, st, x, r, ga, be,
+                             out, sum, a.M, (int)a.C, a.eps);
         });
       });
     return hipGetLastError();
@@ -219,7 +219,9 @@ hipError_t launch_norm_forward(const NormFwd& a, hipStream_t st) {
 
 namespace {
 // workgroups whose waves share the rows of norm_rows_backward
-int64_t norm_groups(int64_t M, int64_t C) { return std::min<int64_t>(C <= 512 ? 1024 : 512, ceil_div(M * norm_row_waves(C), 4)); }
+int64_t norm_groups(int64_t M, int64_t C) {
+  return std::min<int64_t>(C <= 512 ? 1024 : 512, ceil_div(M * norm_row_waves(C), 4));
+}
 size_t norm_sums(const NormBwd& a) {
   const int64_t n = a.C > kNormRowMax ? ceil_div(a.M, chunk_rows(a.M, a.C)) : norm_groups(a.M, a.C);
   return up256((size_t)n * 2 * a.C * sizeof(float));

@@ -11,7 +11,6 @@
 
 namespace afno {
 
-typedef uint32_t u32x4 __attribute__((ext_vector_type(4)));
 enum { kActNone = 0, kActRelu = 1, kActGelu = 2 };
 
 // what happens to a product's element (m, n) on its way out
@@ -171,7 +170,8 @@ struct TilePlace {
     any = (g >> 3) < per && t < all;
     const uint32_t s = t / tiles, i = t - s * tiles, r = i / nc;
     split = (int)s;
-    const uint32_t h0 = nc >= 8 && all >= 1024 ? 8 : 1, first = r / h0 * h0, in = i - first * nc, h = min(h0, (uint32_t)rows - first);
+    const uint32_t h0 = nc >= 8 && all >= 1024 ? 8 : 1, first = r / h0 * h0, in = i - first * nc;
+    const uint32_t h = min(h0, (uint32_t)rows - first);
     n = in / h;
     m = first + (in - in / h * h);
   }

@@ -89,7 +89,8 @@ inline Path product_path(const Product& p, int es) {
   const int ue = 16 / es;
   Path r = {};
   r.rows = !p.ar && p.br && few_rows(p.M, es);
-  r.units = p.lda % ue == 0 && p.ldb % ue == 0 && p.a16 && p.b16 && (!p.ar || p.ma % ue == 0) && (!p.br || p.nb % ue == 0);
+  r.units = p.lda % ue == 0 && p.ldb % ue == 0 && p.a16 && p.b16 && (!p.ar || p.ma % ue == 0) &&
+            (!p.br || p.nb % ue == 0);
   if (!r.rows) r.cut = cut_product(p.M, p.N, p.K, es, r.units);
   return r;
 }

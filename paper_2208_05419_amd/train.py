@@ -219,7 +219,8 @@ def linear_backward(g, x, w, *, pre=None, activation="none", p=0.0, seed=0, offs
         pg, px, pw = _address(g), _address(x), _address(w)
         ws, nbytes, _held = _workspace(x, _bytes(afno_linear_backward_workspace, M, K, N, code,
                                                  _aligned(pg, px, pw)))
-        _check(afno_linear_backward(pg, px, pw, _address(pre), M, K, N, act, *drop, code, _address(dx), _address(dw), _address(db), ws, nbytes, handle))
+        _check(afno_linear_backward(pg, px, pw, _address(pre), M, K, N, act, *drop, code, _address(dx),
+                                    _address(dw), _address(db), ws, nbytes, handle))
         return {"dx": dx, "dw": dw, "db": db}
 
     return _launch(x, stream, (g, x, w, pre, counter), call)
@@ -233,8 +234,9 @@ def layer_norm_forward(x, gamma, beta, *, eps=1e-6, residual=None, out=None, sum
     shape = x.shape
     if gamma is None or beta is None or not _fit(x, (gamma, (C,)), (beta, (C,)), (residual, shape), (out, shape),
                                                  (sum_out, shape)):
-        _expect(x, [("gamma", gamma, (C,), None), ("beta", beta, (C,), None)] + [(n, t, tuple(shape), None) for n, t in (
-            ("residual", residual), ("out", out), ("sum_out", sum_out)) if t is not None])
+        _expect(x, [("gamma", gamma, (C,), None), ("beta", beta, (C,), None)] + [
+            (n, t, tuple(shape), None) for n, t in (("residual", residual), ("out", out), ("sum_out", sum_out))
+            if t is not None])
 
     def call(handle):
         y = x.new_empty(shape) if out is None else out
