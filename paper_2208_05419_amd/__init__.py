@@ -7,10 +7,12 @@ train the rest of an AFNO block (linear products, LayerNorm, dropout); this pack
 Python binding.  Importing it loads nothing; the library is loaded on first use.
 """
 from .afno import (AFNO_ACT_GELU, AFNO_ACT_NONE, AFNO_ACT_RELU,  # noqa: F401
-                   AFNO_DTYPE_BF16, AFNO_DTYPE_FP32, AFNO_ERR_ALIAS, AFNO_ERR_HIP, AFNO_ERR_INVALID_ARG, AFNO_ERR_UNSUPPORTED, AFNO_OK, AFNO_PATH_AUTO,
+                   AFNO_DTYPE_BF16, AFNO_DTYPE_FP32, AFNO_ERR_ALIAS, AFNO_ERR_HIP,
+                   AFNO_ERR_INVALID_ARG, AFNO_ERR_UNSUPPORTED, AFNO_OK, AFNO_PATH_AUTO,
                    AFNO_PATH_GENERIC, AFNO_PATH_VALU_DFT, AFNO_STAGE_DELTA,
                    AFNO_STAGE_MIXED, AFNO_STAGE_SPECTRUM, EXPORTED, LIB_PATH, AfnoError,
-                   BLOCK_PARAMS, KERNELS, afno_block_forward, afno_filter_backward, afno_filter_forward, afno_filter_forward_hidden,
+                   BLOCK_PARAMS, KERNELS, afno_block_forward, afno_filter_backward,
+                   afno_filter_forward, afno_filter_forward_hidden,
                    afno_filter_forward_noalloc, filter_forward_noalloc,
                    afno_filter_stage, afno_filter_stage_hidden,
                    afno_last_error, afno_profile_begin, afno_profile_end, afno_set_kernel_path,

@@ -12,8 +12,8 @@ namespace afno {
 // 2e-37 below, where the exponential leaves the normal numbers; 0.5 z (1 + erf) has 1e-7 to 2e-7
 // for |z| < 1, and below loses all digits by z = -6 to the subtraction.  About 25 issue slots a
 // value where erff takes over 60: the epilogue's values are the exposed part of the block's first
-// product (64,800 x 3072 x 768: 426 us with erff, 387 with this, 320 without any).  |z| is bounded in the tail only (z = +inf gives +inf; -inf and NaN
-// give NaN, as z Phi(z) does).
+// product (64,800 x 3072 x 768: 426 us with erff, 387 with this, 320 without any).  |z| is bounded
+// in the tail only (z = +inf gives +inf; -inf and NaN give NaN, as z Phi(z) does).
 __device__ __forceinline__ float gelu(float z) {
   const float a = fminf(fabsf(z), 16.f);
   const float t = __builtin_amdgcn_rcpf(__builtin_fmaf(0.3f, a, 1.f));

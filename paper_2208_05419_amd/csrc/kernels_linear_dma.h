@@ -224,7 +224,8 @@ __device__ __forceinline__ void dma_store(const GemmArgs<T>& g, const Drop& d, c
 // The two waves of a SIMD belong to two groups (waves 0 to 3 and 4 to 7), and the second runs one
 // barrier behind the first: while one group reads the operands of its next 16 matrix instructions
 // from the LDS, the other has its 16 on the matrix cores, then they change places.  A stage is four such
-// turns (k-halves by row halves).  All waves in step instead: 546 us against 496 (64,800 x 1,024 x 4,096).
+// turns (k-halves by row halves).  All waves of the one workgroup a CU in step instead: 546 us where this then
+// took 496 (64,800 x 1,024 x 4,096).
 // The next stage's loads go out in the first two turns and have to be there at the end of the fourth
 // read, a barrier before the other group begins to read that stage; the buffer that they fill was read
 // for the last time before the barrier ahead of them.

@@ -20,17 +20,19 @@ struct Cut {
   int64_t kper;
 };
 
-// units: the operands are what the direct-to-LDS kernels take.
+// units: the operands are what the direct-to-LDS kernels take.  Times of the present kernels, the join of the
+// splits among them.
 // bf16: 256 where most CUs get a tile of it, also by a split of k that leaves 2,048 to each (64,800 k's, 1,024
-// x 4,096: 520 us in four splits of 256 against 693 in two of 128; 1,080 x 1,536 x 768, 30 tiles: 20 against
-// 8 with 64).  Both: 128 where every CU gets one (bf16, 4,096 x 1,024 x 1,024, 256 tiles: 16.5 us, 64
-// 16.6; 10,368 x 1,536 x 384, 972 tiles: 22 and 32; fp32 from three in four: 10,368 x 384 x 1,536, 243
-// tiles: 116 and 122), or by splits of long sums (bf16, 10,368 k's in 384 x 1,536: 35 us in eight of 128, 41
-// with 64 whole), in fp32 two to a CU where 2,048 k's are left to each (20,000 k's, 2,048 x 2,048: 1,291 us
-// in two splits, 1,549 whole; but 10,368 k's in 384 x 1,536: 123 in seven, 152 in ten).
+// x 4,096: 450 us in four splits of 256, 592 in two of 128; 1,080 x 1,536 x 768, 30 tiles: 21 against
+// 9 with 64).  Both: 128 where every CU gets one (bf16, 10,368 x 1,536 x 384, 972 tiles: 21 us, 64 30; at 256
+// tiles, 4,096 x 1,024 x 1,024, about even: 18.5, 64 16.2 to 17.3), in fp32 from three in four (10,368 x 384 x
+// 1,536, 243 tiles: dw 108, 64 115; but forward and dx 114 and 116, 64 103), or by splits of long sums (bf16,
+// 10,368 k's in 384 x 1,536: 31 us in eight of 128, 41 with 64 whole), in fp32 two to a CU where 2,048 k's are
+// left to each (20,000 k's, 2,048 x 2,048: 1,248 us in two splits, 1,411 whole; but 10,368 k's in 384 x 1,536:
+// 121 in seven, 144 in ten).
 // Else 64, split where the tiles leave CUs without one and the sum is long: a split costs the join's launch,
-// about 3 us, and a stage of k's 0.2 us, in fp32 0.7 (bf16, 256 x 1,024 x 4,096, 64 tiles: 16.6 us whole,
-// 13.0 in four; 64 x 4,096 x 1,024: 6.3 whole, 8.7 in two; fp32 23.7 whole, 12.9 in four).
+// about 3 us, and a stage of k's 0.2 us, in fp32 0.7 (bf16, 256 x 1,024 x 4,096, 64 tiles: 16.7 us whole,
+// 11.4 in four; 64 x 4,096 x 1,024: 6.7 whole, 8.4 in two; fp32 20.5 whole, 13.1 in four).
 // Without units every k-stage waits for its loads: splits until there are two workgroups a CU.
 inline Cut cut_product(int64_t M, int64_t N, int64_t K, int es, bool units) {
   Cut c;
