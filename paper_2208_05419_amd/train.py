@@ -2,7 +2,8 @@
 products with their epilogue, LayerNorm of a residual sum, dropout, each with its gradient.
 
 As in ``afno.py`` this is argument marshalling only.  Tensors are rows of channels with any leading
-shape ([B, H, W, C] grids, [M, C] tokens), float32 or bfloat16, contiguous, on one GPU.
+shape ([B, H, W, C] grids, [M, C] tokens), float32 or bfloat16, contiguous, on one GPU.  With a stream of the
+caller's, the tensors that a call returns are allocated for that stream, and what it reads is recorded on it.
 """
 from __future__ import annotations
 
@@ -197,7 +198,8 @@ def linear_backward(g, x, w, *, pre=None, activation="none", p=0.0, seed=0, offs
     """Gradients of linear_forward for g = dL/dout [..., N] (the residual's gradient is g itself):
     a dict with dx like x, dw like w, db [N], in x's dtype, None where bias, need_dx or need_dw says
     that it is not wanted.  activation, p, seed, offset and the counter's value as in the forward
-    call, pre the tensor that it filled (not read without an activation)."""
+    call, pre the tensor that it filled (not read without an activation).  ReLU passes on 0 where pre is not
+    above 0, whatever g is there."""
     M, K, code = _rows("x", x)
     if w is None or w.dim() != 2:
         raise ValueError("w must be [K, N]")
