@@ -77,8 +77,8 @@ enum {
  * is memory that the graph allocates and frees by itself, and a graph takes one call that does so, of all entry
  * points that allocate (this one, _hidden, _stage, _backward, afno_block_forward): the next one in the same
  * capture returns AFNO_ERR_UNSUPPORTED with nothing recorded, since a replay of several has
- * read memory that was not there any more.  A captured step takes afno_filter_forward_noalloc, any
- * number of times.
+ * read memory that was not there any more.  A captured step takes afno_filter_forward_noalloc, as often
+ * as it needs, one after another.
  * The call is asynchronous: it enqueues on `stream` and returns.
  * B == 0 returns AFNO_OK without touching the GPU (x and out may then be NULL).
  * Errors: arguments are validated before any HIP call; on a non-OK return nothing

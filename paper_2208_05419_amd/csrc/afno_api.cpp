@@ -242,7 +242,7 @@ hipEvent_t* profile_slot() {
 
 // The workspace of a call.  Under capture it is memory that the graph allocates and frees by itself, and a graph
 // gets one such piece: with one in each of several calls of a graph, a kernel of a replay has read its piece
-// when it was not there any more (a GPU fault; each call alone in its graph was right), and the reason
+// when it was not there any more (a GPU fault; the same calls outside of a graph were right), and the reason
 // has not been found.  The captures are told apart by their ids, of which the last 64 are kept.
 int acquire(afno::Workspace& ws, size_t bytes, hipStream_t stream) {
   static std::mutex mu;
