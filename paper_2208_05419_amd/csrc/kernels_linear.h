@@ -479,7 +479,8 @@ __global__ void __launch_bounds__(256) join_splits(const float* __restrict__ par
 // ---------------------------------------------------------------- dz and the bias gradient
 //
 // dz = act'(pre) drop(g), rounded to T for the matrix cores (the one rounding of the backward pass
-// before its results'), rows of ldz values, zeros behind the N of dz; and the sums over chunks of rows of the
+// before its results'; in bf16 it takes dx and dw from 0.0017 to 0.0023 off float64 in the relative 2-norm, where
+// dz in two bf16 terms would double the products, 880 of 1,220 us at 64,800 x 1,024 x 4,096), rows of ldz values, zeros behind the N of dz; and the sums over chunks of rows of the
 // unrounded dz, part [chunks][N].  A workgroup takes the rows of one chunk (blockIdx.y) and 256 columns:
 // 32 threads of eight columns by eight rows at a time, whose sums meet in the LDS.  VEC: N a multiple of 8,
 // g and pre 16-byte aligned.  dz (16-byte aligned, ldz a multiple of 8) or part may be null.
