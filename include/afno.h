@@ -327,6 +327,82 @@ int afno_dropout_backward(const void* g, int64_t n, float p, uint64_t seed, uint
                           const uint64_t* counter, int dtype, void* dx, hipStream_t stream);
 
 /*
+ * The channel MLP in eight bits: rows kept and multiplied in half the memory of bf16, and the
+ * root-mean-square norm that makes them.  Arrays, workspaces, dropout, ownership and errors as for the
+ * operators above.
+ *
+ * Eight bits ("mx8", the Open Compute Project's microscaling layout with E4M3 values): rows of C channels are
+ *   values [M][32 ceil(C / 32)]  uint8, E4M3 (largest 448, no infinity), 0 behind the C channels
+ *   scales [M][ceil(C / 32)]     uint8, s + 127 for every 32 neighbouring channels: a value is 2^s E4M3
+ * with values 16-byte aligned.  Writing, s is the smallest with which no finite value of the block is above
+ * 448 2^s, kept in -117 .. 119 (every value is then a normal bf16 number or 0, and finite: a block with larger
+ * ones has them at 448 2^119), values are rounded to nearest, ties to even, once from float32, and a NaN
+ * or an infinity becomes NaN.  What the calls read has its scales in that range and zeros behind the C.
+ */
+
+/*
+ * afno_mx8_pack -- x [M][C] of dtype to eight bits;  afno_mx8_unpack -- out [M][C] of dtype from
+ * eight bits, exact in either dtype.
+ */
+int afno_mx8_pack(const void* x, int64_t M, int64_t C, int dtype, void* values, void* scales,
+                  hipStream_t stream);
+int afno_mx8_unpack(const void* values, const void* scales, int64_t M, int64_t C, int dtype, void* out,
+                    hipStream_t stream);
+
+/*
+ * afno_rms_norm_forward -- v = x + residual rounded to dtype (residual NULL: v = x);
+ *   out = v / sqrt(mean(v^2) + eps) * gamma over the C channels of a row.
+ *   x, residual [M][C], gamma [C]   dtype;  eps finite and >= 0
+ *   out [M][C] or NULL   dtype;  out_values, out_scales: out in eight bits, or NULL; one of the two at least
+ *   sum [M][C] or NULL   dtype: v, the residual stream and what the gradient takes
+ */
+int afno_rms_norm_forward(const void* x, const void* residual, const void* gamma, int64_t M, int64_t C,
+                          float eps, int dtype, void* out, void* sum, void* out_values,
+                          void* out_scales, hipStream_t stream);
+
+/*
+ * afno_rms_norm_backward -- gradients of the norm of x (the v above) for g = dL/dout (one in eight bits passes
+ * its gradient on as it is):
+ *   with a = g gamma, r = 1 / sqrt(mean(x^2) + eps), h = x r:  dx = r (a - h mean(a h)) + gsum
+ *   dgamma = sum over the rows of g h
+ *   gsum [M][C] or NULL  dtype: the gradient that reaches v along the residual stream
+ *   dx [M][C] dtype; dgamma [C] float32, overwritten.  M == 0: dgamma is 0.
+ */
+int afno_rms_norm_backward(const void* g, const void* x, const void* gamma, const void* gsum, int64_t M,
+                           int64_t C, float eps, int dtype, void* dx, float* dgamma, void* workspace,
+                           int64_t workspace_bytes, hipStream_t stream);
+int64_t afno_rms_norm_backward_workspace(int64_t M, int64_t C, int dtype);
+
+/*
+ * afno_mx8_linear_forward -- out = drop(act(x w^T + b)) + residual for rows in eight bits.
+ *   x [M][K], w [N][K] (output-major: the transpose of afno_linear_forward's)   eight bits
+ *   b [N] or NULL, residual [M][N] or NULL   dtype
+ *   out [M][N] or NULL   dtype;  out_values, out_scales: out in eight bits, or NULL; one of the two at
+ *                        least, each one rounding from the float32 sum
+ *   pre_values, pre_scales   x w^T + b in eight bits, which the gradient of an activation takes, or NULL
+ */
+int afno_mx8_linear_forward(const void* x_values, const void* x_scales, const void* w_values,
+                            const void* w_scales, const void* b, const void* residual, int64_t M,
+                            int64_t K, int64_t N, int activation, float p, uint64_t seed,
+                            uint64_t offset, const uint64_t* counter, int dtype, void* out,
+                            void* out_values, void* out_scales, void* pre_values, void* pre_scales,
+                            void* workspace, int64_t workspace_bytes, hipStream_t stream);
+int64_t afno_mx8_linear_forward_workspace(int64_t M, int64_t K, int64_t N, int dtype);
+
+/*
+ * afno_mx8_linear_backward -- afno_linear_backward from rows kept in eight bits: x and the value before the
+ * activation are what their eight bits stand for, g, w [K][N] (as afno_linear_forward's) and the gradients are
+ * of dtype, the products as afno_linear_backward's.  Where the forward product's w was in eight bits, too, its
+ * rounding passes the gradient on as it is.
+ */
+int afno_mx8_linear_backward(const void* g, const void* x_values, const void* x_scales, const void* w,
+                             const void* pre_values, const void* pre_scales, int64_t M, int64_t K,
+                             int64_t N, int activation, float p, uint64_t seed, uint64_t offset,
+                             const uint64_t* counter, int dtype, void* dx, void* dw, void* db,
+                             void* workspace, int64_t workspace_bytes, hipStream_t stream);
+int64_t afno_mx8_linear_backward_workspace(int64_t M, int64_t K, int64_t N, int dtype, int aligned);
+
+/*
  * Diagnostic per-kernel timing.  afno_profile_begin(max_calls) creates HIP events for
  * up to max_calls filter calls (process-wide); each later afno_filter_forward call
  * records an event before its first kernel and after each of its four phases, on the

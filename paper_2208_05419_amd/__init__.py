@@ -3,8 +3,8 @@
 The filter (forward real 2-D FFT of a [B,H,W,C] token grid, block-diagonal complex MLP
 per Fourier mode, softshrink, hard mode cutoff, inverse real FFT, residual add) runs in
 hand-written HIP kernels behind the C ABI of ``include/afno.h``, and so do the operators that
-train the rest of an AFNO block (linear products, LayerNorm, dropout); this package is its
-Python binding.  Importing it loads nothing; the library is loaded on first use.
+train the rest of an AFNO block (linear products, LayerNorm, dropout) and those that keep and multiply
+its rows in eight bits; this package is its Python binding.  Importing it loads nothing; the library is loaded on first use.
 """
 from .afno import (AFNO_ACT_GELU, AFNO_ACT_NONE, AFNO_ACT_RELU,  # noqa: F401
                    AFNO_DTYPE_BF16, AFNO_DTYPE_FP32, AFNO_ERR_ALIAS, AFNO_ERR_HIP,
@@ -24,3 +24,8 @@ from .train import (ACTIVATIONS, afno_dropout_backward, afno_dropout_forward,  #
                     afno_layer_norm_forward, afno_linear_backward, afno_linear_backward_workspace,
                     afno_linear_forward, afno_linear_forward_workspace, dropout_backward,
                     dropout_forward, layer_norm_backward, layer_norm_forward, linear_backward, linear_forward)
+from .mx8 import (Mx8, afno_mx8_linear_backward, afno_mx8_linear_backward_workspace,  # noqa: F401
+                  afno_mx8_linear_forward, afno_mx8_linear_forward_workspace, afno_mx8_pack, afno_mx8_unpack,
+                  afno_rms_norm_backward, afno_rms_norm_backward_workspace, afno_rms_norm_forward, mx8_empty,
+                  mx8_linear_backward, mx8_linear_forward, mx8_pack, mx8_unpack, rms_norm_backward,
+                  rms_norm_forward)

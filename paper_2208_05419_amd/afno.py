@@ -38,6 +38,9 @@ EXPORTED = ("afno_filter_forward", "afno_filter_forward_noalloc", "afno_filter_f
             "afno_layer_norm_backward", "afno_dropout_forward", "afno_dropout_backward",
             "afno_linear_forward_workspace", "afno_linear_backward_workspace",
             "afno_layer_norm_backward_workspace",
+            "afno_mx8_pack", "afno_mx8_unpack", "afno_rms_norm_forward", "afno_rms_norm_backward",
+            "afno_rms_norm_backward_workspace", "afno_mx8_linear_forward", "afno_mx8_linear_backward",
+            "afno_mx8_linear_forward_workspace", "afno_mx8_linear_backward_workspace",
             "afno_profile_begin", "afno_profile_end", "afno_set_kernel_path", "afno_last_error",
             "afno_version")
 KERNELS = ("prep", "row_r2c", "column", "row_c2r")
@@ -108,6 +111,20 @@ def load_library():
     lib.afno_linear_backward_workspace.argtypes = [i64, i64, i64, ci, ci]
     lib.afno_layer_norm_backward_workspace.argtypes = [i64, i64, ci]
     for name in ("linear_forward", "linear_backward", "layer_norm_backward"):
+        getattr(lib, f"afno_{name}_workspace").restype = i64
+    lib.afno_mx8_pack.argtypes = [vp, i64, i64, ci, vp, vp, vp]
+    lib.afno_mx8_unpack.argtypes = [vp, vp, i64, i64, ci, vp, vp]
+    lib.afno_rms_norm_forward.argtypes = [vp] * 3 + [i64, i64, f32, ci] + [vp] * 5
+    lib.afno_rms_norm_backward.argtypes = [vp] * 4 + [i64, i64, f32, ci] + [vp] * 3 + [i64, vp]
+    lib.afno_mx8_linear_forward.argtypes = [vp] * 6 + [i64] * 3 + [ci] + drop + [ci] + [vp] * 6 + [i64, vp]
+    lib.afno_mx8_linear_backward.argtypes = [vp] * 6 + [i64] * 3 + [ci] + drop + [ci] + [vp] * 4 + [i64, vp]
+    for name in ("mx8_pack", "mx8_unpack", "rms_norm_forward", "rms_norm_backward", "mx8_linear_forward",
+                 "mx8_linear_backward"):
+        getattr(lib, "afno_" + name).restype = ci
+    lib.afno_rms_norm_backward_workspace.argtypes = [i64, i64, ci]
+    lib.afno_mx8_linear_forward_workspace.argtypes = [i64, i64, i64, ci]
+    lib.afno_mx8_linear_backward_workspace.argtypes = [i64, i64, i64, ci, ci]
+    for name in ("rms_norm_backward", "mx8_linear_forward", "mx8_linear_backward"):
         getattr(lib, f"afno_{name}_workspace").restype = i64
     lib.afno_last_error.argtypes = []
     lib.afno_last_error.restype = ctypes.c_char_p

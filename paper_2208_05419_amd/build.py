@@ -21,11 +21,12 @@ FLAGS = [
 
 
 # (source, its own flags): compiled side by side, then linked.  afno_kernels.hip and
-# afno_api.cpp alone make the same library (afno_rows.hip and afno_train.hip are then part of the
-# first).
+# afno_api.cpp alone make the same library (afno_rows.hip, afno_train.hip and afno_mx8.hip are then part
+# of the first).
 UNITS = [(os.path.join(CSRC, "afno_kernels.hip"), ["-DAFNO_SEPARATE_ROWS"])] + [
     (os.path.join(CSRC, "afno_rows.hip"), [f"-DAFNO_ROWS_PART={p}"]) for p in range(4)
-] + [(os.path.join(CSRC, "afno_train.hip"), []), (os.path.join(CSRC, "afno_api.cpp"), [])]
+] + [(os.path.join(CSRC, "afno_train.hip"), []), (os.path.join(CSRC, "afno_mx8.hip"), []),
+     (os.path.join(CSRC, "afno_api.cpp"), [])]
 
 
 def build(verbose: bool = False, extra=()) -> str:

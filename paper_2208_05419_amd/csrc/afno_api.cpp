@@ -615,3 +615,4 @@ int afno_version(void) { return 100; }
 }  // extern "C"
 
 #include "afno_api_train.h"
+#include "afno_api_mx8.h"

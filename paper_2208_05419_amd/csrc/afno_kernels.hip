@@ -29,6 +29,7 @@
 #ifndef AFNO_SEPARATE_ROWS
 #include "afno_rows.hip"
 #include "afno_train.hip"
+#include "afno_mx8.hip"
 #endif
 #include "kernels_fast.h"
 #include "kernels_generic.h"

@@ -4,25 +4,16 @@
 #include <stdint.h>
 
 #include <algorithm>
-#include <type_traits>
 
 #include "kernels_linear_dma.h"
 #include "kernels_norm.h"
+#include "launch_util.h"
 #include "linear_rules.h"
+#include "mx8_internal.h"
 #include "train_internal.h"
 
 namespace afno {
 namespace {
-
-template <typename F>
-auto by_type(int dtype, F f) {
-  return dtype == 0 ? f(float()) : f(bf16());
-}
-template <typename F>
-auto by_flag(bool v, F f) {
-  return v ? f(std::true_type()) : f(std::false_type());
-}
-bool at16(const void* p) { return ((uintptr_t)p & 15) == 0; }  // null counts as aligned
 
 __global__ void zero_kernel(uint16_t* p, size_t n) {
   for (size_t i = (size_t)blockIdx.x * 256 + threadIdx.x; i < n; i += (size_t)gridDim.x * 256) p[i] = 0;
@@ -85,7 +76,7 @@ LinearSizes sizes_of(const LinearFwd& a) {
 }
 LinearSizes sizes_of(const LinearBwd& a) {
   return {a.M, a.K, a.N, a.dtype == 0 ? 4 : 2, at16(a.x), at16(a.w), at16(a.g), a.dx != nullptr, a.dw != nullptr,
-          a.db != nullptr, a.act != kActNone || a.drop.threshold != 0};
+          a.db != nullptr, a.act != kActNone || a.drop.threshold != 0, a.x8.q != nullptr};
 }
 
 }  // namespace
@@ -139,15 +130,21 @@ hipError_t launch_linear_backward(const LinearBwd& a, void* ws, hipStream_t st) 
     float* sums = reinterpret_cast<float*>(base + l.sums);
     float* part = reinterpret_cast<float*>(base + l.part);
     PackArgs<T> px = {}, pw = {};
-    if (l.copy_x) px = {x, reinterpret_cast<T*>(base + l.x), a.M, a.K, l.kp};
+    if (l.copy_x) px = {x, reinterpret_cast<T*>(base + l.x), a.x8.q ? 0 : a.M, a.K, l.kp};
     if (l.copy_w) pw = {w, reinterpret_cast<T*>(base + l.w), a.K, a.N, l.np};
     pack(px, pw, st);
+    if (a.x8.q && a.dw) {
+      const hipError_t e = launch_unpack8(a.x8, px.dst, l.kp, a.M, a.dtype, st);
+      if (e != hipSuccess) return e;
+    }
     if (l.need_dz || a.db) {
       const int64_t rows = chunk_rows(a.M, a.N), chunks = ceil_div(a.M, rows);
       by_flag(a.N % 8 == 0 && at16(g) && at16(pre), [&](auto v) {
-        hipLaunchKernelGGL((dz_kernel<T, decltype(v)::value>),
-                           dim3((unsigned)ceil_div(a.N, 256), (unsigned)chunks), dim3(256), 0, st, g, pre,
-                           dzw, l.np, a.db ? sums : nullptr, a.M, a.N, rows, a.act, a.drop);
+        by_flag(a.pre8.q != nullptr, [&](auto p8) {
+          hipLaunchKernelGGL((dz_kernel<T, decltype(v)::value, decltype(p8)::value>),
+                             dim3((unsigned)ceil_div(a.N, 256), (unsigned)chunks), dim3(256), 0, st, g, pre, a.pre8,
+                             dzw, l.np, a.db ? sums : nullptr, a.M, a.N, rows, a.act, a.drop);
+        });
       });
       if (a.db)
         hipLaunchKernelGGL((join_columns<T>), dim3((unsigned)ceil_div(a.N, 16)), dim3(1024), 0, st, sums,
@@ -177,26 +174,6 @@ hipError_t launch_linear_backward(const LinearBwd& a, void* ws, hipStream_t st) 
 }
 
 // ---------------------------------------------------------------- LayerNorm
-
-namespace {
-// the kernels that hold a row in registers, by the channels that they have room for and the waves that
-// share a row: all of a row's loads are under way at once, and fewer registers leave more rows to a CU.  From
-// 1,025 to 2,048 channels one wave holds a row (295 to 368 registers backward), which serves many rows: of 64,800,
-// backward 170 us against 259 with four waves (1,152 bf16), 256 and 267 (2,048 bf16), 407 and 425 (fp32), forward
-// 106 and 113, 191 and 175, 386 and 365.  Few rows leave CUs to it half empty: 5,187 x 2,048 backward 50 against 34
-// (fp32 53 and 35), 500 x 2,048 18.3 and 17.2, forward about even.
-template <typename F>
-void by_capacity(int64_t C, F f) {
-  const auto one = std::integral_constant<int, 1>();
-  const auto four = std::integral_constant<int, 4>();
-  if (C <= 512) f(std::integral_constant<int, 512>(), one);
-  else if (C <= 1024) f(std::integral_constant<int, 1024>(), one);
-  else if (C <= 2048) f(std::integral_constant<int, 2048>(), one);
-  else if (C <= 4096) f(std::integral_constant<int, 4096>(), four);
-  else f(std::integral_constant<int, kNormRowMax>(), four);
-}
-int64_t norm_row_waves(int64_t C) { return C <= 2048 ? 1 : 4; }
-}  // namespace
 
 hipError_t launch_norm_forward(const NormFwd& a, hipStream_t st) {
   return by_type(a.dtype, [&](auto z) {

@@ -8,6 +8,7 @@
 #include "dropout.h"
 #include "gelu.h"
 #include "kernel_common.h"
+#include "mx8.h"
 
 namespace afno {
 
@@ -487,8 +488,9 @@ __global__ void __launch_bounds__(256) join_splits(const float* __restrict__ par
 // Bound by the vector ALUs and memory alike: 64,800 x 4,096 bf16 with GELU and dropout 327 us for 1.6 GB
 // (4.9 TB/s), 243 without the store of dz, 92 for the sums of g alone; the activation chosen once for eight
 // values, 337 with the choice at each value.  The next rows' loads under way meanwhile: 330, not kept.
-template <typename T, bool VEC>
-__global__ void __launch_bounds__(256) dz_kernel(const T* __restrict__ g, const T* __restrict__ pre,
+// PRE8: the value before the activation is in eight bits, pre8 (mx8.h), and not in pre.
+template <typename T, bool VEC, bool PRE8 = false>
+__global__ void __launch_bounds__(256) dz_kernel(const T* __restrict__ g, const T* __restrict__ pre, Rows8 pre8,
                                                  T* __restrict__ dz, int64_t ldz, float* __restrict__ part,
                                                  int64_t M, int64_t N, int64_t rows, int act, DropArgs da) {
   __shared__ float sums[8][256];
@@ -504,7 +506,14 @@ __global__ void __launch_bounds__(256) dz_kernel(const T* __restrict__ g, const 
       union { uint4 u[NU]; T e[8]; } gv, pv, ov;
 #pragma unroll
       for (int i = 0; i < NU; ++i) gv.u[i] = Unit<T>::template load<VEC>(g + at + UE * i, N - n - UE * i);
-      if (act) {
+      uint2 p8 = make_uint2(0, 0);
+      float scale = 0.f;
+      if constexpr (PRE8) {
+        if (act) {
+          p8 = *reinterpret_cast<const uint2*>(pre8.q + m * pre8.ld + n);
+          scale = power8(pre8.s[m * (pre8.ld / kBlock8) + n / kBlock8]);
+        }
+      } else if (act) {
 #pragma unroll
         for (int i = 0; i < NU; ++i) pv.u[i] = Unit<T>::template load<VEC>(pre + at + UE * i, N - n - UE * i);
       }
@@ -520,12 +529,20 @@ __global__ void __launch_bounds__(256) dz_kernel(const T* __restrict__ g, const 
           d.apply_from(v, (uint64_t)at);
         }
       }
+      float z[8];
+      if constexpr (PRE8) {
+        widen8(p8.x, scale, z);
+        widen8(p8.y, scale, z + 4);
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) z[j] = (float)pv.e[j];
+      }
       if (act == kActGelu) {
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] *= gelu_grad((float)pv.e[j]);
+        for (int j = 0; j < 8; ++j) v[j] *= gelu_grad(z[j]);
       } else if (act == kActRelu) {  // selected: an infinity at a unit that is off is no NaN
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = (float)pv.e[j] > 0.f ? v[j] : 0.f;
+        for (int j = 0; j < 8; ++j) v[j] = z[j] > 0.f ? v[j] : 0.f;
       }
 #pragma unroll
       for (int j = 0; j < 8; ++j) {

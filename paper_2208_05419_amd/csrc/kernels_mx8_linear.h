@@ -1,0 +1,425 @@
+// kernels_mx8_linear.h -- products of rows in eight bits (mx8.h) with their epilogue:
+//   out = drop(act(x w + b)) + residual,   x [M][K], w [N][K] (output-major: both k-major)
+// out in the storage type, in eight bits or both, and x w + b in eight bits.
+//
+// bf16: the matrix cores' scaled instruction, which multiplies 16 x 16 tiles over 128 k's of E4M3 values and
+// applies the scales of x and w itself, at twice the rate of bf16.  v_mfma_scale_f32_16x16x128_f8f6f4: lane
+// l = 16 gq + l16 gives of row l16 the k's 16 gq .. + 15 and 64 + 16 gq .. + 15 (measured: with a byte of one lane set and the
+// scales of all lanes distinct), and the scale of that row's block gq, k's 32 gq .. + 31.  Its sums are in float32 but
+// for one place: of eight neighbouring k's products the instruction drops what lies below 2^-13 of the
+// power of two in the largest (measured: 1 + 2^-13 is kept, 1 + 2^-14 is not, nor any number of them; the unscaled
+// instruction does so too), 1.7e-5 of the result in the relative 2-norm at any K where bfloat16 rounds off 1.7e-3 and E4M3 2.6e-2.
+//
+// fp32, which that would cost seven bits: the values and scales as bfloat16, which holds each of them, on the bf16
+// instruction, whose products and sums lose nothing beyond float32's own roundings (6e-8 at 2,048 k's), at half the rate.
+#pragma once
+#include "kernels_linear_dma.h"
+#include "mx8.h"
+
+namespace afno {
+
+typedef int i32x8 __attribute__((ext_vector_type(8)));
+// a lane's operand of a stage: 32 values of a row
+union Mx8Op {
+  uint4 u[2];
+  uint32_t w[8];
+  i32x8 v;
+};
+// acc += the products of a stage's operands under their scale bytes, transposed
+template <typename T, int TM, int TN, int AM>
+__device__ __forceinline__ void mx8_products(const Mx8Op (&fa)[TM], const Mx8Op (&fb)[TN], const int* sa,
+                                             const int* sb, f32x4 (&acc)[AM][TN], int a0) {
+  if constexpr (sizeof(T) == 2) {
+#pragma unroll
+    for (int a = 0; a < TM; ++a)
+#pragma unroll
+      for (int b = 0; b < TN; ++b)
+        acc[a0 + a][b] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(fb[b].v, fa[a].v, acc[a0 + a][b], 0, 0, 0,
+                                                                          sb[b], 0, sa[a]);
+  } else {
+#pragma unroll
+    for (int s = 0; s < 4; ++s) {
+      union Wide { uint2 h[2]; bf16x8 v; } wa[TM], wb[TN];
+#pragma unroll
+      for (int b = 0; b < TN; ++b)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) wb[b].h[i] = widen8_bf16(fb[b].w[2 * s + i], power8(sb[b]));
+#pragma unroll
+      for (int a = 0; a < TM; ++a)
+#pragma unroll
+        for (int i = 0; i < 2; ++i) wa[a].h[i] = widen8_bf16(fa[a].w[2 * s + i], power8(sa[a]));
+#pragma unroll
+      for (int a = 0; a < TM; ++a)
+#pragma unroll
+        for (int b = 0; b < TN; ++b)
+          acc[a0 + a][b] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wb[b].v, wa[a].v, acc[a0 + a][b], 0, 0, 0);
+    }
+  }
+}
+
+template <typename T>
+struct Mx8Args {
+  const uint8_t *a, *as, *b, *bs;  // values [M][ld], [N][ld], scales [..][ld / 32]
+  int64_t M, N, ld;
+  int64_t kper;  // k of one split, a multiple of 128
+  int splits;
+  float* part;   // [splits][M][N] sums (splits > 1), else null
+  Epilogue<T> e; // out may be null; pre is
+  Rows8 out8, pre8;
+};
+
+// W rows of a stage's 128 k's as a slab in the LDS: rows of 128 bytes, the 16-byte chunk c of row r at place
+// c ^ f(r), so that the rows that a pass of ds_read_b128 takes cover the banks once.  A wave takes the WAVE rows
+// from WAVE * its place.  B: the second operand, whose rows are dealt to the tiles of 16 so that in the
+// transposed product a lane ends up with eight neighbouring columns of every 32: tile b, lane l16 = 4 r + c has
+// row 32 (b / 2) + 8 r + 4 (b % 2) + c.
+// WIDE: a lane's two chunks of a row are a block's, 2 gq and 2 gq + 1, and not gq and 4 + gq, so that one scale widens
+// both.
+template <bool B, bool WIDE, int W, int WAVE, int NT>
+struct Slab8 {
+  static constexpr int CH = 8, U = W * CH, L = U / NT;  // chunks of a row, 16-byte units, loads a lane
+  static_assert(U % NT == 0, "whole loads");
+  const uint8_t* base;  // the workgroup's first row
+  uint32_t at[L];       // this lane's loads, bytes behind a stage's base
+  int v[2];             // this lane's operand places, bytes into the slab
+  Buf scales;           // of the workgroup's rows
+  uint32_t sat[WAVE / 16];  // this lane's scale of each tile's first block
+
+  __device__ static __forceinline__ int swizzle(int i) { return B ? (i & 3) | ((i >> 1) & 4) : i & 7; }
+  __device__ __forceinline__ Slab8(const uint8_t* q, const uint8_t* s, int64_t ld, int64_t o, int64_t rows, int tid,
+                                   int wave)
+      : base(q + o * ld),
+        scales(s + o * (ld / kBlock8), (uint32_t)(min((int64_t)W, rows - o) * (ld / kBlock8))) {
+    const int64_t left = rows - o;  // rows behind the last read that one, for products that are not stored
+#pragma unroll
+    for (int j = 0; j < L; ++j) {
+      const int u = tid + NT * j, r = u / CH, c = (u % CH) ^ swizzle(r);
+      at[j] = (uint32_t)min((int64_t)r, left - 1) * (uint32_t)ld + 16 * c;
+    }
+    const int lane = tid & 63, l16 = lane & 15, gq = lane >> 4;
+    const int r = WAVE * wave + (B ? 8 * (l16 >> 2) + (l16 & 3) : l16);
+#pragma unroll
+    for (int h = 0; h < 2; ++h) v[h] = 16 * (r * CH + ((WIDE ? 2 * gq + h : 4 * h + gq) ^ swizzle(r)));
+#pragma unroll
+    for (int t = 0; t < WAVE / 16; ++t) {
+      const int64_t row = r + (B ? 32 * (t >> 1) + 4 * (t & 1) : 16 * t);
+      sat[t] = (uint32_t)min(row, left - 1) * (uint32_t)(ld / kBlock8) + gq;
+    }
+  }
+  // the loads of the whole stage from k on; d: the slab + 64 * wave
+  __device__ __forceinline__ void issue(uint4* d, int64_t k) const {
+    const char* s = reinterpret_cast<const char*>(base) + k;
+#pragma unroll
+    for (int j = 0; j < L; ++j) lds_load16(s + at[j], d + NT * j);
+  }
+  // the last `left` k's, fewer than a stage, and zeros
+  __device__ __forceinline__ void issue_rest(uint4* d, int64_t k, int left, int tid) const {
+    const char* s = reinterpret_cast<const char*>(base) + k;
+#pragma unroll
+    for (int j = 0; j < L; ++j) {
+      const int u = tid + NT * j;
+      if (16 * ((u % CH) ^ swizzle(u / CH)) < left) lds_load16(s + at[j], d + NT * j);
+      else d[NT * j + (tid & 63)] = make_uint4(0, 0, 0, 0);
+    }
+  }
+  // tile t's operand
+  __device__ __forceinline__ Mx8Op read(const uint4* slab, int t) const {
+    const char* p = reinterpret_cast<const char*>(slab) + (B ? 4096 * (t >> 1) + 512 * (t & 1) : 2048 * t);
+    Mx8Op o;
+    o.u[0] = *reinterpret_cast<const uint4*>(p + v[0]);
+    o.u[1] = *reinterpret_cast<const uint4*>(p + v[1]);
+    return o;
+  }
+  // tile t's scale byte for the stage at k; any power for the blocks behind its `left` k's, where all values are 0
+  __device__ __forceinline__ int scale(int64_t k, int t, int gq, int left) const {
+    const bool there = 32 * gq < left;
+    const int v = (int)__builtin_amdgcn_raw_buffer_load_b8(scales.r, there ? sat[t] : sat[t] - gq,
+                                                           (uint32_t)(k / kBlock8), 0);
+    return there ? v : 127;
+  }
+};
+
+// Eight neighbouring values of row m from column n on, a whole block in four lanes of the wave, which all
+// call this together: LANES 4: neighbouring ones, 64: lanes l + 16 i.  there: the row and the first column
+// exist (columns behind the last are not stored).
+template <int LANES>
+__device__ __forceinline__ void store8(const Rows8& o, int64_t m, int64_t n, int64_t N, const float (&z)[8],
+                                       bool there) {
+  float v[8], top = 0.f;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    v[i] = n + i < N ? z[i] : 0.f;
+    top = fmaxf(top, size8(v[i]));
+  }
+  const int byte = scale8(LANES == 4 ? lanes_max<4>(top) : rows_max(top));
+  uint32_t w[2];
+  round8(v, byte, w);
+  if (!there || n >= o.ld) return;
+  typedef uint32_t Words __attribute__((ext_vector_type(2)));
+  __builtin_nontemporal_store((Words){w[0], w[1]}, reinterpret_cast<Words*>(o.q + m * o.ld + n));
+  if (n % kBlock8 == 0) o.s[m * (o.ld / kBlock8) + n / kBlock8] = (uint8_t)byte;
+}
+
+// The epilogue of eight neighbouring values, bias[] theirs; as store8 all lanes of the wave together.
+template <typename T, int LANES>
+__device__ __forceinline__ void finish8(const Mx8Args<T>& g, const Drop& d, int64_t m, int64_t n,
+                                        const float (&bias)[8], float (&o)[8], bool units) {
+  const Epilogue<T>& e = g.e;
+  const bool there = m < g.M, whole = there && n + 8 <= g.N;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) o[i] += bias[i];
+  if (g.pre8.q) store8<LANES>(g.pre8, m, n, g.N, o, there);
+  if (e.act == kActGelu) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = gelu(o[i]);
+  } else if (e.act == kActRelu) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] = activate(o[i], kActRelu);
+  }
+  const int64_t at = m * g.N + n;
+  if (d.threshold) {
+    if (g.N % 8 == 0) {
+      const uint4 w = d.numbers((uint64_t)at >> 3);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) o[i] = d.apply(o[i], w, i);
+    } else {
+      d.apply_from(o, (uint64_t)at);
+    }
+  }
+  constexpr int NV = 16 / sizeof(T), NU = 8 / NV;
+  if (e.residual) {
+    union { uint4 u[NU]; T e[8]; } r;
+#pragma unroll
+    for (int i = 0; i < NU; ++i)
+      r.u[i] = Unit<T>::template load<false>(e.residual + at + NV * i, there ? g.N - n - NV * i : 0);
+#pragma unroll
+    for (int i = 0; i < 8; ++i) o[i] += (float)r.e[i];
+  }
+  if (e.out) {
+    union { uint4 u[NU]; T e[8]; uint32_t w[NU][4]; } r;
+    typedef uint32_t Words __attribute__((ext_vector_type(4)));
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r.e[i] = Store<T>::to(o[i]);
+    if (whole && units) {
+#pragma unroll
+      for (int i = 0; i < NU; ++i)
+        __builtin_nontemporal_store((Words){r.w[i][0], r.w[i][1], r.w[i][2], r.w[i][3]},
+                                    reinterpret_cast<Words*>(e.out + at + NV * i));
+    } else if (whole) {
+      __builtin_memcpy(e.out + at, &r, sizeof(r));
+    } else if (there) {
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (n + i < g.N) e.out[at + i] = r.e[i];
+    }
+  }
+  if (g.out8.q) store8<LANES>(g.out8, m, n, g.N, o, there);
+}
+template <typename T>
+__device__ __forceinline__ void load_bias8(const Epilogue<T>& e, int64_t N, int64_t n, float (&b)[8]) {
+  constexpr int NV = 16 / sizeof(T);
+  union { uint4 u[8 / NV]; T e[8]; } r;
+#pragma unroll
+  for (int i = 0; i < 8 / NV; ++i)
+    r.u[i] = Unit<T>::template load<false>(e.bias + n + NV * i, e.bias ? N - n - NV * i : 0);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) b[i] = (float)r.e[i];
+}
+
+// The epilogue of a wave's TM x TN tiles without LDS: this lane has row l16 of every 16 and columns 8 gq .. + 7 of
+// every 32.  m0, n0: the wave's first row and column.
+template <typename T, int TM, int TN>
+__device__ __forceinline__ void mx8_store(const Mx8Args<T>& g, const Drop& d, const f32x4 (&acc)[TM][TN],
+                                          int64_t m0, int64_t n0, int split, int lane) {
+  const int l16 = lane & 15, gq = lane >> 4;
+  const bool units = (uintptr_t)g.e.out % 16 == 0 && g.N % (16 / sizeof(T)) == 0;
+  float bias[TN / 2][8];  // all loads at once
+#pragma unroll
+  for (int h = 0; h < TN / 2; ++h) load_bias8(g.e, g.N, n0 + 8 * gq + 32 * h, bias[h]);
+#pragma unroll
+  for (int h = 0; h < TN / 2; ++h) {
+    const int64_t n = n0 + 8 * gq + 32 * h;
+    if (n0 + 32 * h >= g.N) continue;  // the whole wave's
+#pragma unroll
+    for (int a = 0; a < TM; ++a) {
+      const int64_t m = m0 + 16 * a + l16;
+      __builtin_amdgcn_sched_barrier(0);  // one group's values at a time in registers
+      float o[8];
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        o[q] = acc[a][2 * h][q];
+        o[4 + q] = acc[a][2 * h + 1][q];
+      }
+      if (!g.part) {
+        finish8<T, 64>(g, d, m, n, bias[h], o, units);
+        continue;
+      }
+      if (m >= g.M) continue;
+      float* p = g.part + (split * g.M + m) * g.N + n;
+      if (g.N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (n + 4 * i < g.N)
+            *reinterpret_cast<float4*>(p + 4 * i) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+      } else {
+#pragma unroll
+        for (int e = 0; e < 8; ++e)
+          if (n + e < g.N) p[e] = o[e];
+      }
+    }
+  }
+}
+
+// Workgroup tile TILE x TILE (128 or 64), 4 waves as 2 x 2, stages of 128 k's in two (four) LDS buffers of 32 KB
+// (16 KB), the next stages' loads under way during the present one's products.
+template <typename T, int TILE>
+__global__ void __launch_bounds__(256) mx8_gemm_tile(Mx8Args<T> g) {
+  constexpr int NT = 256, WR = TILE / 2, TM = WR / 16, TN = WR / 16, NS = TILE == 128 ? 2 : 4;
+  constexpr bool WIDE = sizeof(T) == 4;
+  typedef Slab8<false, WIDE, TILE, WR, NT> SA;
+  typedef Slab8<true, WIDE, TILE, WR, NT> SB;
+  constexpr int U = SA::U + SB::U, BK = 128;
+  __shared__ uint4 st0[U];
+  __shared__ uint4 st1[U];
+  __shared__ uint4 st2[NS == 4 ? U : 1];
+  __shared__ uint4 st3[NS == 4 ? U : 1];
+  const TilePlace t((g.M + TILE - 1) / TILE, (g.N + TILE - 1) / TILE, g.splits);
+  if (!t.any) return;
+  const int64_t m0 = t.m * TILE, n0 = t.n * TILE;
+  const int64_t k0 = t.split * g.kper, k1 = min(g.ld, k0 + g.kper);
+  const int tid = threadIdx.x, lane = tid & 63, gq = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 1, wn = wave & 1;
+  const int S = (int)((k1 - k0) / BK), left = (int)(k1 - k0 - (int64_t)S * BK);  // whole stages, the rest
+  const SA sa(g.a, g.as, g.ld, m0, g.M, tid, wm);
+  const SB sb(g.b, g.bs, g.ld, n0, g.N, tid, wn);
+
+  f32x4 acc[TM][TN];
+#pragma unroll
+  for (int a = 0; a < TM; ++a)
+#pragma unroll
+    for (int b = 0; b < TN; ++b) acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  struct Scales { int a[TM], b[TN]; };
+  auto fetch = [&](Scales& s, int64_t k, int n) {
+#pragma unroll
+    for (int a = 0; a < TM; ++a) s.a[a] = sa.scale(k, a, gq, n);
+#pragma unroll
+    for (int b = 0; b < TN; ++b) s.b[b] = sb.scale(k, b, gq, n);
+  };
+  auto issue = [&](uint4* st, Scales& s, int i) {
+    const int64_t k = k0 + (int64_t)min(i, S - 1) * BK;  // behind the last: that one again, nobody reads it
+    fetch(s, k, BK);
+    sa.issue(st + 64 * wave, k);
+    sb.issue(st + SA::U + 64 * wave, k);
+  };
+  auto compute = [&](const uint4* st, const Scales& s) {
+    Mx8Op fa[TM], fb[TN];
+#pragma unroll
+    for (int b = 0; b < TN; ++b) fb[b] = sb.read(st + SA::U, b);
+#pragma unroll
+    for (int a = 0; a < TM; ++a) fa[a] = sa.read(st, a);
+    mx8_products<T>(fa, fb, s.a, s.b, acc, 0);
+  };
+  constexpr int L = SA::L + SB::L + TM + TN;  // loads of a stage
+  // this wave's loads of the present stage there (the later ones may be under way), its reads of the last
+  // one done, then every wave's
+  auto sync = [&]() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(kWaitLds);
+    __builtin_amdgcn_s_waitcnt(wait_loads((NS - 2) * L));
+    dma_barrier();
+  };
+  auto sync_all = [&]() {
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(kWaitAll);
+    dma_barrier();
+  };
+  Scales s0, s1, s2, s3;
+  if (S) {
+    issue(st0, s0, 0);
+    if constexpr (NS == 4) {
+      issue(st1, s1, 1);
+      issue(st2, s2, 2);
+    }
+  }
+  const Drop d(g.e.drop);
+  if (S) {
+    int s = 0;
+    if constexpr (NS == 2) {
+      for (; s + 1 < S; s += 2) {
+        sync();
+        issue(st1, s1, s + 1);
+        compute(st0, s0);
+        sync();
+        issue(st0, s0, s + 2);
+        compute(st1, s1);
+      }
+      sync_all();
+      if (S & 1) compute(st0, s0);
+    } else {
+      for (; s + 3 < S; s += 4) {
+        sync();
+        issue(st3, s3, s + 3);
+        compute(st0, s0);
+        sync();
+        issue(st0, s0, s + 4);
+        compute(st1, s1);
+        sync();
+        issue(st1, s1, s + 5);
+        compute(st2, s2);
+        sync();
+        issue(st2, s2, s + 6);
+        compute(st3, s3);
+      }
+      sync_all();
+      if (S - s > 0) compute(st0, s0);
+      if (S - s > 1) compute(st1, s1);
+      if (S - s > 2) compute(st2, s2);
+    }
+  }
+  if (left > 0) {
+    // a buffer that no wave reads any more: the last that may be is st2, or st0 of two
+    uint4* rest = NS == 2 ? st1 : st3;
+    if (S) sync_all();
+    const int64_t k = k0 + (int64_t)S * BK;
+    fetch(s0, k, left);
+    sa.issue_rest(rest + 64 * wave, k, left, tid);
+    sb.issue_rest(rest + SA::U + 64 * wave, k, left, tid);
+    sync_all();
+    compute(rest, s0);
+  }
+  mx8_store<T, TM, TN>(g, d, acc, m0 + WR * wm, n0 + WR * wn, t.split, lane);
+}
+
+// The splits' sums added in order, then the epilogue; eight neighbouring elements a thread, four threads a block.
+template <typename T>
+__global__ void __launch_bounds__(256) mx8_join_splits(Mx8Args<T> g) {
+  const int64_t per = row8(g.N) / 8, t = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t m = t / per, n = 8 * (t - m * per);
+  float v[8] = {0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f, 0.f};
+  if (m < g.M) {
+    const float* p = g.part + m * g.N + n;
+    for (int s = 0; s < g.splits; ++s, p += g.M * g.N) {
+      if (g.N % 4 == 0) {
+#pragma unroll
+        for (int i = 0; i < 2; ++i)
+          if (n + 4 * i < g.N) {
+            const float4 w = *reinterpret_cast<const float4*>(p + 4 * i);
+            v[4 * i] += w.x;
+            v[4 * i + 1] += w.y;
+            v[4 * i + 2] += w.z;
+            v[4 * i + 3] += w.w;
+          }
+      } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j)
+          if (n + j < g.N) v[j] += p[j];
+      }
+    }
+  }
+  const Drop d(g.e.drop);
+  float bias[8];
+  load_bias8(g.e, g.N, n, bias);
+  finish8<T, 4>(g, d, m, n, bias, v, (uintptr_t)g.e.out % 16 == 0 && g.N % (16 / sizeof(T)) == 0);
+}
+
+}  // namespace afno

@@ -121,6 +121,7 @@ struct LinearSizes {
   int64_t M, K, N;
   int es;
   bool x16, w16, g16, dx, dw, db, factor;
+  bool x8 = false;  // x is in eight bits: dw takes a copy in the storage type
 };
 // Its workspace: copies of operands that are no 16-byte units (whatever the addresses turn out to be,
 // room for them where the sizes are worth it), the factor dz, chunk sums, the splits' sums.
@@ -149,7 +150,7 @@ inline Layout backward_layout(const LinearSizes& a) {
   l.np = packing ? ceil_div(a.N, 8) * 8 : a.N;
   l.need_dz = (a.dx || a.dw) && (a.factor || (packing && (l.np != a.N || !a.g16)));
   if (l.need_dz) l.np = ceil_div(a.N, 8) * 8;
-  l.copy_x = packing && a.dw && (l.kp != a.K || !a.x16);
+  l.copy_x = a.dw && (a.x8 || (packing && (l.kp != a.K || !a.x16)));
   l.copy_w = packing && a.dx && (l.np != a.N || !a.w16);
   l.w = l.copy_x ? up256((size_t)a.M * l.kp * a.es) : 0;
   l.dz = l.w + (l.copy_w ? up256((size_t)a.K * l.np * a.es) : 0);

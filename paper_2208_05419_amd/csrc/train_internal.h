@@ -6,6 +6,7 @@
 #include <stdint.h>
 
 #include "dropout.h"
+#include "mx8.h"
 
 namespace afno {
 
@@ -24,6 +25,7 @@ struct LinearBwd {
   int act, dtype;
   DropArgs drop;
   void *dx, *dw, *db;
+  Rows8 x8 = {}, pre8 = {};  // x and pre in eight bits (then x and pre are null), or null
 };
 struct NormFwd {
   const void *x, *residual, *gamma, *beta;
