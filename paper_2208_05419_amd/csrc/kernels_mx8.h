@@ -23,13 +23,10 @@ __global__ void __launch_bounds__(256) mx8_pack_kernel(const T* __restrict__ x, 
     union { uint4 u[NU]; T e[8]; } xv;
 #pragma unroll
     for (int i = 0; i < NU; ++i) xv.u[i] = Unit<T>::template load<false>(x + m * C + c + UE * i, C - c - UE * i);
-    float v[8], top = 0.f;
+    float v[8];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
-      v[i] = (float)xv.e[i];
-      top = fmaxf(top, size8(v[i]));
-    }
-    const int byte = scale8(lanes_max<4>(top));
+    for (int i = 0; i < 8; ++i) v[i] = (float)xv.e[i];
+    const int byte = block_scale8(v, [](float top) { return lanes_max<4>(top); });
     uint32_t w[2];
     round8(v, byte, w);
     *reinterpret_cast<uint2*>(o.q + m * o.ld + c) = make_uint2(w[0], w[1]);
@@ -87,10 +84,7 @@ __device__ __forceinline__ float row_rms(const float (&v)[NU][UE], int C, float 
 // UE neighbouring values of each of the 32 / UE lanes of a block, to eight bits at channel c of a row
 template <int UE>
 __device__ __forceinline__ void put8(const Rows8& o, int64_t m, int64_t c, const float (&v)[UE], bool there) {
-  float top = 0.f;
-#pragma unroll
-  for (int e = 0; e < UE; ++e) top = fmaxf(top, size8(v[e]));
-  const int byte = scale8(lanes_max<kBlock8 / UE>(top));
+  const int byte = block_scale8(v, [](float top) { return lanes_max<kBlock8 / UE>(top); });
   uint32_t w[(UE + 3) / 4];
   round8(v, byte, w);
   if (!there) return;

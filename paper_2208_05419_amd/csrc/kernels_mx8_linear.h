@@ -25,6 +25,11 @@ union Mx8Op {
   uint32_t w[8];
   i32x8 v;
 };
+// a scale byte as mx8_products takes it: the scaled instruction looks at the lowest byte alone
+template <typename T>
+__device__ __forceinline__ int scale_byte(uint32_t w) {
+  return (int)(sizeof(T) == 2 ? w : w & 255);
+}
 // acc += the products of a stage's operands under their scale bytes, transposed
 template <typename T, int TM, int TN, int AM>
 __device__ __forceinline__ void mx8_products(const Mx8Op (&fa)[TM], const Mx8Op (&fb)[TN], const int* sa,
@@ -82,14 +87,14 @@ struct Slab8 {
   const uint8_t* base;  // the workgroup's first row
   uint32_t at[L];       // this lane's loads, bytes behind a stage's base
   int v[2];             // this lane's operand places, bytes into the slab
-  Buf scales;           // of the workgroup's rows
-  uint32_t sat[WAVE / 16];  // this lane's scale of each tile's first block
+  const uint8_t* scales;    // of the workgroup's first row
+  uint32_t sat[WAVE / 16];  // this lane's row of each tile in them
 
   __device__ static __forceinline__ int swizzle(int i) { return B ? (i & 3) | ((i >> 1) & 4) : i & 7; }
   __device__ __forceinline__ Slab8(const uint8_t* q, const uint8_t* s, int64_t ld, int64_t o, int64_t rows, int tid,
                                    int wave)
       : base(q + o * ld),
-        scales(s + o * (ld / kBlock8), (uint32_t)(min((int64_t)W, rows - o) * (ld / kBlock8))) {
+        scales(s + o * (ld / kBlock8)) {
     const int64_t left = rows - o;  // rows behind the last read that one, for products that are not stored
 #pragma unroll
     for (int j = 0; j < L; ++j) {
@@ -103,7 +108,7 @@ struct Slab8 {
 #pragma unroll
     for (int t = 0; t < WAVE / 16; ++t) {
       const int64_t row = r + (B ? 32 * (t >> 1) + 4 * (t & 1) : 16 * t);
-      sat[t] = (uint32_t)min(row, left - 1) * (uint32_t)(ld / kBlock8) + gq;
+      sat[t] = (uint32_t)min(row, left - 1) * (uint32_t)(ld / kBlock8);
     }
   }
   // the loads of the whole stage from k on; d: the slab + 64 * wave
@@ -130,14 +135,30 @@ struct Slab8 {
     o.u[1] = *reinterpret_cast<const uint4*>(p + v[1]);
     return o;
   }
-  // tile t's scale byte for the stage at k; any power for the blocks behind its `left` k's, where all values are 0
-  __device__ __forceinline__ int scale(int64_t k, int t, int gq, int left) const {
+  // tile t's scale byte for the stage at k, of which only `left` k's are there; any power for the blocks behind
+  // them, where all values are 0
+  __device__ __forceinline__ int rest_scale(int64_t k, int t, int gq, int left) const {
     const bool there = 32 * gq < left;
-    const int v = (int)__builtin_amdgcn_raw_buffer_load_b8(scales.r, there ? sat[t] : sat[t] - gq,
-                                                           (uint32_t)(k / kBlock8), 0);
+    const int v = scales[sat[t] + (there ? gq : 0) + (uint32_t)(k / kBlock8)];
     return there ? v : 127;
   }
+  // tile t's scale bytes of four stages from k on in one load: lane group gq gets the four blocks of stage gq (of
+  // `stages` that are there: of the last one else)
+  __device__ __forceinline__ uint32_t four_scales(int64_t k, int t, int gq, int stages) const {
+    uint32_t w;
+    __builtin_memcpy(&w, scales + sat[t] + (uint32_t)(k / kBlock8) + 4 * min(gq, stages - 1), 4);
+    return w;
+  }
 };
+
+// four_scales' words of the four lane groups turned round: byte j of lane group gq is block gq of stage j
+__device__ __forceinline__ uint32_t turn_scales(uint32_t w, uint32_t sel) {
+  const auto h = __builtin_amdgcn_permlane32_swap(w, w, false, false);            // of gq % 2, of gq % 2 + 2
+  const auto a = __builtin_amdgcn_permlane16_swap(h[0], h[0], false, false);      // of 0, of 1
+  const auto b = __builtin_amdgcn_permlane16_swap(h[1], h[1], false, false);      // of 2, of 3
+  return __builtin_amdgcn_perm(__builtin_amdgcn_perm(b[1], b[0], sel), __builtin_amdgcn_perm(a[1], a[0], sel),
+                               0x05040100u);
+}
 
 // Eight neighbouring values of row m from column n on, a whole block in four lanes of the wave, which all
 // call this together: LANES 4: neighbouring ones, 64: lanes l + 16 i.  there: the row and the first column
@@ -145,13 +166,14 @@ struct Slab8 {
 template <int LANES>
 __device__ __forceinline__ void store8(const Rows8& o, int64_t m, int64_t n, int64_t N, const float (&z)[8],
                                        bool there) {
-  float v[8], top = 0.f;
+  float v[8];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) {
-    v[i] = n + i < N ? z[i] : 0.f;
-    top = fmaxf(top, size8(v[i]));
+  for (int i = 0; i < 8; ++i) v[i] = z[i];
+  if (N % kBlock8) {
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = n + i < N ? z[i] : 0.f;
   }
-  const int byte = scale8(LANES == 4 ? lanes_max<4>(top) : rows_max(top));
+  const int byte = block_scale8(v, [](float top) { return LANES == 4 ? lanes_max<4>(top) : rows_max(top); });
   uint32_t w[2];
   round8(v, byte, w);
   if (!there || n >= o.ld) return;
@@ -298,28 +320,45 @@ __global__ void __launch_bounds__(256) mx8_gemm_tile(Mx8Args<T> g) {
   for (int a = 0; a < TM; ++a)
 #pragma unroll
     for (int b = 0; b < TN; ++b) acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
-  struct Scales { int a[TM], b[TN]; };
-  auto fetch = [&](Scales& s, int64_t k, int n) {
+  // four stages' scales: those in use, and the next four's words under way
+  uint32_t pa[TM], pb[TN], ra[TM], rb[TN];
+  const uint32_t sel = (uint32_t)(gq | (4 + gq) << 8);
+  auto fetch = [&](int i) {  // of stages i .. i + 3
+    const int64_t k = k0 + (int64_t)min(i, S - 1) * BK;
 #pragma unroll
-    for (int a = 0; a < TM; ++a) s.a[a] = sa.scale(k, a, gq, n);
+    for (int a = 0; a < TM; ++a) ra[a] = sa.four_scales(k, a, gq, max(1, S - i));
 #pragma unroll
-    for (int b = 0; b < TN; ++b) s.b[b] = sb.scale(k, b, gq, n);
+    for (int b = 0; b < TN; ++b) rb[b] = sb.four_scales(k, b, gq, max(1, S - i));
   };
-  auto issue = [&](uint4* st, Scales& s, int i) {
+  auto issue = [&](uint4* st, int i) {
     const int64_t k = k0 + (int64_t)min(i, S - 1) * BK;  // behind the last: that one again, nobody reads it
-    fetch(s, k, BK);
     sa.issue(st + 64 * wave, k);
     sb.issue(st + SA::U + 64 * wave, k);
   };
-  auto compute = [&](const uint4* st, const Scales& s) {
+  auto products = [&](const uint4* st, const int (&ca)[TM], const int (&cb)[TN]) {
     Mx8Op fa[TM], fb[TN];
 #pragma unroll
     for (int b = 0; b < TN; ++b) fb[b] = sb.read(st + SA::U, b);
 #pragma unroll
     for (int a = 0; a < TM; ++a) fa[a] = sa.read(st, a);
-    mx8_products<T>(fa, fb, s.a, s.b, acc, 0);
+    mx8_products<T>(fa, fb, ca, cb, acc, 0);
   };
-  constexpr int L = SA::L + SB::L + TM + TN;  // loads of a stage
+  auto compute = [&](const uint4* st, int i) {  // stage i
+    if ((i & 3) == 0) {
+#pragma unroll
+      for (int a = 0; a < TM; ++a) pa[a] = turn_scales(ra[a], sel);
+#pragma unroll
+      for (int b = 0; b < TN; ++b) pb[b] = turn_scales(rb[b], sel);
+      fetch(i + 4);
+    }
+    int ca[TM], cb[TN];
+#pragma unroll
+    for (int a = 0; a < TM; ++a) ca[a] = scale_byte<T>(pa[a] >> 8 * (i & 3));
+#pragma unroll
+    for (int b = 0; b < TN; ++b) cb[b] = scale_byte<T>(pb[b] >> 8 * (i & 3));
+    products(st, ca, cb);
+  };
+  constexpr int L = SA::L + SB::L;  // loads of a stage, apart from scales
   // this wave's loads of the present stage there (the later ones may be under way), its reads of the last
   // one done, then every wave's
   auto sync = [&]() {
@@ -333,12 +372,12 @@ __global__ void __launch_bounds__(256) mx8_gemm_tile(Mx8Args<T> g) {
     __builtin_amdgcn_s_waitcnt(kWaitAll);
     dma_barrier();
   };
-  Scales s0, s1, s2, s3;
   if (S) {
-    issue(st0, s0, 0);
+    fetch(0);
+    issue(st0, 0);
     if constexpr (NS == 4) {
-      issue(st1, s1, 1);
-      issue(st2, s2, 2);
+      issue(st1, 1);
+      issue(st2, 2);
     }
   }
   const Drop d(g.e.drop);
@@ -347,33 +386,33 @@ __global__ void __launch_bounds__(256) mx8_gemm_tile(Mx8Args<T> g) {
     if constexpr (NS == 2) {
       for (; s + 1 < S; s += 2) {
         sync();
-        issue(st1, s1, s + 1);
-        compute(st0, s0);
+        issue(st1, s + 1);
+        compute(st0, s);
         sync();
-        issue(st0, s0, s + 2);
-        compute(st1, s1);
+        issue(st0, s + 2);
+        compute(st1, s + 1);
       }
       sync_all();
-      if (S & 1) compute(st0, s0);
+      if (S & 1) compute(st0, s);
     } else {
       for (; s + 3 < S; s += 4) {
         sync();
-        issue(st3, s3, s + 3);
-        compute(st0, s0);
+        issue(st3, s + 3);
+        compute(st0, s);
         sync();
-        issue(st0, s0, s + 4);
-        compute(st1, s1);
+        issue(st0, s + 4);
+        compute(st1, s + 1);
         sync();
-        issue(st1, s1, s + 5);
-        compute(st2, s2);
+        issue(st1, s + 5);
+        compute(st2, s + 2);
         sync();
-        issue(st2, s2, s + 6);
-        compute(st3, s3);
+        issue(st2, s + 6);
+        compute(st3, s + 3);
       }
       sync_all();
-      if (S - s > 0) compute(st0, s0);
-      if (S - s > 1) compute(st1, s1);
-      if (S - s > 2) compute(st2, s2);
+      if (S - s > 0) compute(st0, s);
+      if (S - s > 1) compute(st1, s + 1);
+      if (S - s > 2) compute(st2, s + 2);
     }
   }
   if (left > 0) {
@@ -381,11 +420,15 @@ __global__ void __launch_bounds__(256) mx8_gemm_tile(Mx8Args<T> g) {
     uint4* rest = NS == 2 ? st1 : st3;
     if (S) sync_all();
     const int64_t k = k0 + (int64_t)S * BK;
-    fetch(s0, k, left);
+    int ca[TM], cb[TN];
+#pragma unroll
+    for (int a = 0; a < TM; ++a) ca[a] = sa.rest_scale(k, a, gq, left);
+#pragma unroll
+    for (int b = 0; b < TN; ++b) cb[b] = sb.rest_scale(k, b, gq, left);
     sa.issue_rest(rest + 64 * wave, k, left, tid);
     sb.issue_rest(rest + SA::U + 64 * wave, k, left, tid);
     sync_all();
-    compute(rest, s0);
+    products(rest, ca, cb);
   }
   mx8_store<T, TM, TN>(g, d, acc, m0 + WR * wm, n0 + WR * wn, t.split, lane);
 }

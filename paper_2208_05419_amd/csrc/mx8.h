@@ -23,10 +23,23 @@ struct Rows8 {
   int64_t ld;
 };
 
-// |v|, 0 for a NaN or an infinity: what the choice of a scale looks at
-__device__ __forceinline__ float size8(float v) {
-  const float a = fabsf(v);
-  return a < __builtin_inff() ? a : 0.f;
+// the largest size of N values and `top`; a NaN says nothing
+template <int N>
+__device__ __forceinline__ float largest8(const float (&v)[N], float top) {
+#pragma unroll
+  for (int i = 0; i < N; ++i) top = fmaxf(top, fabsf(v[i]));
+  return top;
+}
+// the same of the finite ones, where an infinity is among them
+template <int N>
+__device__ __forceinline__ float largest_finite8(const float (&v)[N]) {
+  float top = 0.f;
+#pragma unroll
+  for (int i = 0; i < N; ++i) {
+    const float a = fabsf(v[i]);
+    top = fmaxf(top, a < __builtin_inff() ? a : 0.f);
+  }
+  return top;
 }
 // the scale byte for values of which `top` is the largest in size
 __device__ __forceinline__ int scale8(float top) {
@@ -100,6 +113,16 @@ __device__ __forceinline__ float rows_max(float v) {
   v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
   const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   return fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+
+// The scale byte of a block whose values lie in several lanes, N in each, JOIN the largest over them: all lanes of
+// the wave together.  Infinities are looked for only in a wave that has one.
+template <int N, typename F>
+__device__ __forceinline__ int block_scale8(const float (&v)[N], F join) {
+  float top = join(largest8(v, 0.f));
+  if (__builtin_amdgcn_ballot_w64(top == __builtin_inff())) top = join(largest_finite8(v));
+  return scale8(top);
 }
 
 }  // namespace afno
