@@ -76,8 +76,8 @@ struct Mx8Args {
 // W rows of a stage's 128 k's as a slab in the LDS: rows of 128 bytes, the 16-byte chunk c of row r at place
 // c ^ f(r), so that the rows that a pass of ds_read_b128 takes cover the banks once.  A wave takes the WAVE rows
 // from WAVE * its place.  B: the second operand, whose rows are dealt to the tiles of 16 so that in the
-// transposed product a lane ends up with eight neighbouring columns of every 32: tile b, lane l16 = 4 r + c has
-// row 32 (b / 2) + 8 r + 4 (b % 2) + c.
+// transposed product a lane ends up with NV = WAVE / 4 neighbouring columns (16, the 16 bytes of a store in eight bits,
+// or 8): tile b, lane l16 = 4 r + c has row NV r + 4 b + c.
 // WIDE: a lane's two chunks of a row are a block's, 2 gq and 2 gq + 1, and not gq and 4 + gq, so that one scale widens
 // both.
 template <bool B, bool WIDE, int W, int WAVE, int NT>
@@ -90,7 +90,8 @@ struct Slab8 {
   const uint8_t* scales;    // of the workgroup's first row
   uint32_t sat[WAVE / 16];  // this lane's row of each tile in them
 
-  __device__ static __forceinline__ int swizzle(int i) { return B ? (i & 3) | ((i >> 1) & 4) : i & 7; }
+  static constexpr int NV = WAVE / 4;
+  __device__ static __forceinline__ int swizzle(int i) { return B ? (i & 3) | (i / (NV / 4) & 4) : i & 7; }
   __device__ __forceinline__ Slab8(const uint8_t* q, const uint8_t* s, int64_t ld, int64_t o, int64_t rows, int tid,
                                    int wave)
       : base(q + o * ld),
@@ -102,12 +103,12 @@ struct Slab8 {
       at[j] = (uint32_t)min((int64_t)r, left - 1) * (uint32_t)ld + 16 * c;
     }
     const int lane = tid & 63, l16 = lane & 15, gq = lane >> 4;
-    const int r = WAVE * wave + (B ? 8 * (l16 >> 2) + (l16 & 3) : l16);
+    const int r = WAVE * wave + (B ? NV * (l16 >> 2) + (l16 & 3) : l16);
 #pragma unroll
     for (int h = 0; h < 2; ++h) v[h] = 16 * (r * CH + ((WIDE ? 2 * gq + h : 4 * h + gq) ^ swizzle(r)));
 #pragma unroll
     for (int t = 0; t < WAVE / 16; ++t) {
-      const int64_t row = r + (B ? 32 * (t >> 1) + 4 * (t & 1) : 16 * t);
+      const int64_t row = r + (B ? 4 : 16) * t;
       sat[t] = (uint32_t)min(row, left - 1) * (uint32_t)(ld / kBlock8);
     }
   }
@@ -129,7 +130,7 @@ struct Slab8 {
   }
   // tile t's operand
   __device__ __forceinline__ Mx8Op read(const uint4* slab, int t) const {
-    const char* p = reinterpret_cast<const char*>(slab) + (B ? 4096 * (t >> 1) + 512 * (t & 1) : 2048 * t);
+    const char* p = reinterpret_cast<const char*>(slab) + (B ? 512 : 2048) * t;
     Mx8Op o;
     o.u[0] = *reinterpret_cast<const uint4*>(p + v[0]);
     o.u[1] = *reinterpret_cast<const uint4*>(p + v[1]);
@@ -160,134 +161,152 @@ __device__ __forceinline__ uint32_t turn_scales(uint32_t w, uint32_t sel) {
                                0x05040100u);
 }
 
-// Eight neighbouring values of row m from column n on, a whole block in four lanes of the wave, which all
-// call this together: LANES 4: neighbouring ones, 64: lanes l + 16 i.  there: the row and the first column
-// exist (columns behind the last are not stored).
-template <int LANES>
-__device__ __forceinline__ void store8(const Rows8& o, int64_t m, int64_t n, int64_t N, const float (&z)[8],
+// NV (8 or 16) neighbouring values of row m from column n on, in eight bits; JOIN, the lanes of a block: all lanes of
+// the wave together.  there: the row exists (columns behind the last are not stored).
+enum { kNeighbours, kRowsApart };
+template <int NV, int JOIN>
+__device__ __forceinline__ void store8(const Rows8& o, int64_t m, int64_t n, int64_t N, const float (&z)[NV],
                                        bool there) {
-  float v[8];
+  float v[NV];
 #pragma unroll
-  for (int i = 0; i < 8; ++i) v[i] = z[i];
+  for (int i = 0; i < NV; ++i) v[i] = z[i];
   if (N % kBlock8) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) v[i] = n + i < N ? z[i] : 0.f;
+    for (int i = 0; i < NV; ++i) v[i] = n + i < N ? z[i] : 0.f;
   }
-  const int byte = block_scale8(v, [](float top) { return LANES == 4 ? lanes_max<4>(top) : rows_max(top); });
-  uint32_t w[2];
+  constexpr int LANES = kBlock8 / NV;
+  const int byte =
+      block_scale8(v, [](float top) { return JOIN == kNeighbours ? lanes_max<LANES>(top) : rows_max<LANES>(top); });
+  uint32_t w[NV / 4];
   round8(v, byte, w);
   if (!there || n >= o.ld) return;
-  typedef uint32_t Words __attribute__((ext_vector_type(2)));
-  __builtin_nontemporal_store((Words){w[0], w[1]}, reinterpret_cast<Words*>(o.q + m * o.ld + n));
+  typedef uint32_t Words __attribute__((ext_vector_type(NV / 4)));
+  Words u;
+#pragma unroll
+  for (int i = 0; i < NV / 4; ++i) u[i] = w[i];
+  *reinterpret_cast<Words*>(o.q + m * o.ld + n) = u;
   if (n % kBlock8 == 0) o.s[m * (o.ld / kBlock8) + n / kBlock8] = (uint8_t)byte;
 }
 
-// The epilogue of eight neighbouring values, bias[] theirs; as store8 all lanes of the wave together.
-template <typename T, int LANES>
-__device__ __forceinline__ void finish8(const Mx8Args<T>& g, const Drop& d, int64_t m, int64_t n,
-                                        const float (&bias)[8], float (&o)[8], bool units) {
-  const Epilogue<T>& e = g.e;
-  const bool there = m < g.M, whole = there && n + 8 <= g.N;
+// NV values of type T in registers
+template <typename T, int NV>
+union Some {
+  static constexpr int UE = 16 / sizeof(T), NU = NV / UE;
+  uint4 u[NU];
+  T e[NV];
+  // p[0 .. n), 0 behind them, at any address
+  __device__ __forceinline__ void load(const T* p, int64_t n) {
 #pragma unroll
-  for (int i = 0; i < 8; ++i) o[i] += bias[i];
-  if (g.pre8.q) store8<LANES>(g.pre8, m, n, g.N, o, there);
+    for (int i = 0; i < NU; ++i) u[i] = Unit<T>::template load<false>(p + UE * i, n - UE * i);
+  }
+};
+
+// The epilogue of NV neighbouring values, bias[] theirs; as store8 all lanes of the wave together.
+template <typename T, int NV, int JOIN>
+__device__ __forceinline__ void finish8(const Mx8Args<T>& g, const Drop& d, int64_t m, int64_t n,
+                                        const float (&bias)[NV], float (&o)[NV], bool units) {
+  const Epilogue<T>& e = g.e;
+  const bool there = m < g.M;
+#pragma unroll
+  for (int i = 0; i < NV; ++i) o[i] += bias[i];
+  if (g.pre8.q) store8<NV, JOIN>(g.pre8, m, n, g.N, o, there);
   if (e.act == kActGelu) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = gelu(o[i]);
+    for (int i = 0; i < NV; ++i) o[i] = gelu(o[i]);
   } else if (e.act == kActRelu) {
 #pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] = activate(o[i], kActRelu);
+    for (int i = 0; i < NV; ++i) o[i] = activate(o[i], kActRelu);
   }
   const int64_t at = m * g.N + n;
   if (d.threshold) {
-    if (g.N % 8 == 0) {
-      const uint4 w = d.numbers((uint64_t)at >> 3);
 #pragma unroll
-      for (int i = 0; i < 8; ++i) o[i] = d.apply(o[i], w, i);
-    } else {
-      d.apply_from(o, (uint64_t)at);
+    for (int h = 0; h < NV / 8; ++h) {
+      float(&v)[8] = *reinterpret_cast<float(*)[8]>(o + 8 * h);
+      if (g.N % 8 == 0) {
+        const uint4 w = d.numbers(((uint64_t)at >> 3) + h);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) v[i] = d.apply(v[i], w, i);
+      } else {
+        d.apply_from(v, (uint64_t)at + 8 * h);
+      }
     }
   }
-  constexpr int NV = 16 / sizeof(T), NU = 8 / NV;
+  typedef Some<T, NV> S;
   if (e.residual) {
-    union { uint4 u[NU]; T e[8]; } r;
+    S r;
+    r.load(e.residual + at, there ? g.N - n : 0);
 #pragma unroll
-    for (int i = 0; i < NU; ++i)
-      r.u[i] = Unit<T>::template load<false>(e.residual + at + NV * i, there ? g.N - n - NV * i : 0);
-#pragma unroll
-    for (int i = 0; i < 8; ++i) o[i] += (float)r.e[i];
+    for (int i = 0; i < NV; ++i) o[i] += (float)r.e[i];
   }
   if (e.out) {
-    union { uint4 u[NU]; T e[8]; uint32_t w[NU][4]; } r;
-    typedef uint32_t Words __attribute__((ext_vector_type(4)));
+    S r;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) r.e[i] = Store<T>::to(o[i]);
-    if (whole && units) {
+    for (int i = 0; i < NV; ++i) r.e[i] = Store<T>::to(o[i]);
+    if (there && n + NV <= g.N) {
+      typedef uint32_t Words __attribute__((ext_vector_type(4)));
 #pragma unroll
-      for (int i = 0; i < NU; ++i)
-        __builtin_nontemporal_store((Words){r.w[i][0], r.w[i][1], r.w[i][2], r.w[i][3]},
-                                    reinterpret_cast<Words*>(e.out + at + NV * i));
-    } else if (whole) {
-      __builtin_memcpy(e.out + at, &r, sizeof(r));
+      for (int i = 0; i < S::NU; ++i) {
+        if (units)
+          __builtin_nontemporal_store((Words){r.u[i].x, r.u[i].y, r.u[i].z, r.u[i].w},
+                                      reinterpret_cast<Words*>(e.out + at + S::UE * i));
+        else
+          __builtin_memcpy(e.out + at + S::UE * i, &r.u[i], 16);
+      }
     } else if (there) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
+      for (int i = 0; i < NV; ++i)
         if (n + i < g.N) e.out[at + i] = r.e[i];
     }
   }
-  if (g.out8.q) store8<LANES>(g.out8, m, n, g.N, o, there);
+  if (g.out8.q) store8<NV, JOIN>(g.out8, m, n, g.N, o, there);
 }
+template <typename T, int NV>
+__device__ __forceinline__ void load_bias8(const Epilogue<T>& e, int64_t N, int64_t n, float (&b)[NV]) {
+  Some<T, NV> r;
+  r.load(e.bias + n, e.bias ? N - n : 0);
+#pragma unroll
+  for (int i = 0; i < NV; ++i) b[i] = (float)r.e[i];
+}
+// whether out takes 16-byte stores
 template <typename T>
-__device__ __forceinline__ void load_bias8(const Epilogue<T>& e, int64_t N, int64_t n, float (&b)[8]) {
-  constexpr int NV = 16 / sizeof(T);
-  union { uint4 u[8 / NV]; T e[8]; } r;
-#pragma unroll
-  for (int i = 0; i < 8 / NV; ++i)
-    r.u[i] = Unit<T>::template load<false>(e.bias + n + NV * i, e.bias ? N - n - NV * i : 0);
-#pragma unroll
-  for (int i = 0; i < 8; ++i) b[i] = (float)r.e[i];
+__device__ __forceinline__ bool whole_units8(const Mx8Args<T>& g) {
+  return (uintptr_t)g.e.out % 16 == 0 && g.N % (16 / sizeof(T)) == 0;
 }
 
-// The epilogue of a wave's TM x TN tiles without LDS: this lane has row l16 of every 16 and columns 8 gq .. + 7 of
-// every 32.  m0, n0: the wave's first row and column.
+// The epilogue of a wave's TM x TN tiles without LDS: this lane has row l16 of every 16 and 4 TN neighbouring
+// columns.  m0, n0: the wave's first row and column.
 template <typename T, int TM, int TN>
 __device__ __forceinline__ void mx8_store(const Mx8Args<T>& g, const Drop& d, const f32x4 (&acc)[TM][TN],
                                           int64_t m0, int64_t n0, int split, int lane) {
+  constexpr int NV = 4 * TN;
+  if (n0 >= g.N) return;  // the whole wave's
   const int l16 = lane & 15, gq = lane >> 4;
-  const bool units = (uintptr_t)g.e.out % 16 == 0 && g.N % (16 / sizeof(T)) == 0;
-  float bias[TN / 2][8];  // all loads at once
+  const bool units = whole_units8(g);
+  const int64_t n = n0 + NV * gq;
+  float bias[NV];
+  load_bias8(g.e, g.N, n, bias);
 #pragma unroll
-  for (int h = 0; h < TN / 2; ++h) load_bias8(g.e, g.N, n0 + 8 * gq + 32 * h, bias[h]);
+  for (int a = 0; a < TM; ++a) {
+    const int64_t m = m0 + 16 * a + l16;
+    __builtin_amdgcn_sched_barrier(0);  // one group's values at a time in registers
+    float o[NV];
 #pragma unroll
-  for (int h = 0; h < TN / 2; ++h) {
-    const int64_t n = n0 + 8 * gq + 32 * h;
-    if (n0 + 32 * h >= g.N) continue;  // the whole wave's
+    for (int i = 0; i < NV; ++i) o[i] = acc[a][i / 4][i % 4];
+    if (!g.part) {
+      finish8<T, NV, kRowsApart>(g, d, m, n, bias, o, units);
+      continue;
+    }
+    if (m >= g.M) continue;
+    float* p = g.part + (split * g.M + m) * g.N + n;
+    if (g.N % 4 == 0) {
 #pragma unroll
-    for (int a = 0; a < TM; ++a) {
-      const int64_t m = m0 + 16 * a + l16;
-      __builtin_amdgcn_sched_barrier(0);  // one group's values at a time in registers
-      float o[8];
+      for (int i = 0; i < TN; ++i)
+        if (n + 4 * i < g.N)
+          *reinterpret_cast<float4*>(p + 4 * i) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+    } else {
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        o[q] = acc[a][2 * h][q];
-        o[4 + q] = acc[a][2 * h + 1][q];
-      }
-      if (!g.part) {
-        finish8<T, 64>(g, d, m, n, bias[h], o, units);
-        continue;
-      }
-      if (m >= g.M) continue;
-      float* p = g.part + (split * g.M + m) * g.N + n;
-      if (g.N % 4 == 0) {
-#pragma unroll
-        for (int i = 0; i < 2; ++i)
-          if (n + 4 * i < g.N)
-            *reinterpret_cast<float4*>(p + 4 * i) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 8; ++e)
-          if (n + e < g.N) p[e] = o[e];
-      }
+      for (int e = 0; e < NV; ++e)
+        if (n + e < g.N) p[e] = o[e];
     }
   }
 }
@@ -462,7 +481,7 @@ __global__ void __launch_bounds__(256) mx8_join_splits(Mx8Args<T> g) {
   const Drop d(g.e.drop);
   float bias[8];
   load_bias8(g.e, g.N, n, bias);
-  finish8<T, 4>(g, d, m, n, bias, v, (uintptr_t)g.e.out % 16 == 0 && g.N % (16 / sizeof(T)) == 0);
+  finish8<T, 8, kNeighbours>(g, d, m, n, bias, v, whole_units8(g));
 }
 
 }  // namespace afno
