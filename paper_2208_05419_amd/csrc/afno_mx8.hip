@@ -117,12 +117,12 @@ hipError_t launch_rms_backward(const RmsBwd& a, void* ws, hipStream_t st) {
 
 // ---------------------------------------------------------------- products
 
-size_t mx8_forward_bytes(const Mx8Fwd& a) { return mx8_part_bytes(a.M, a.N, a.x.ld); }
+size_t mx8_forward_bytes(const Mx8Fwd& a) { return mx8_part_bytes(a.M, a.N, a.x.ld, a.dtype == 0 ? 4 : 2); }
 
 hipError_t launch_mx8_forward(const Mx8Fwd& a, void* ws, hipStream_t st) {
   return by_type(a.dtype, [&](auto z) {
     typedef decltype(z) T;
-    const Cut c = cut_mx8(a.M, a.N, a.x.ld);
+    const Cut c = cut_mx8(a.M, a.N, a.x.ld, (int)sizeof(T));
     Mx8Args<T> g = {};
     g.a = a.x.q;
     g.as = a.x.s;
@@ -139,7 +139,9 @@ hipError_t launch_mx8_forward(const Mx8Fwd& a, void* ws, hipStream_t st) {
     g.out8 = a.out8;
     g.pre8 = a.pre8;
     const dim3 grid((unsigned)(8 * ceil_div(c.splits * ceil_div(g.M, c.tile) * ceil_div(g.N, c.tile), 8)));
-    if (c.tile == 128) hipLaunchKernelGGL((mx8_gemm_tile<T, 128>), grid, dim3(256), 0, st, g);
+    if (c.tile == 256) {
+      if constexpr (sizeof(T) == 2) hipLaunchKernelGGL(mx8_gemm_tile256, grid, dim3(512), 0, st, g);
+    } else if (c.tile == 128) hipLaunchKernelGGL((mx8_gemm_tile<T, 128>), grid, dim3(256), 0, st, g);
     else hipLaunchKernelGGL((mx8_gemm_tile<T, 64>), grid, dim3(256), 0, st, g);
     if (c.splits > 1)
       hipLaunchKernelGGL((mx8_join_splits<T>), dim3((unsigned)ceil_div(g.M * (row8(g.N) / 8), 256)), dim3(256), 0, st,

@@ -85,10 +85,10 @@ struct Slab8 {
   static constexpr int CH = 8, U = W * CH, L = U / NT;  // chunks of a row, 16-byte units, loads a lane
   static_assert(U % NT == 0, "whole loads");
   const uint8_t* base;  // the workgroup's first row
-  uint32_t at[L];       // this lane's loads, bytes behind a stage's base
-  int v[2];             // this lane's operand places, bytes into the slab
-  const uint8_t* scales;    // of the workgroup's first row
-  uint32_t sat[WAVE / 16];  // this lane's row of each tile in them
+  uint32_t at, last, far;  // this lane's first load, bytes behind a stage's base, its place in the last row; from load to load
+  int v[2];                // this lane's operand places, bytes into the slab
+  const uint8_t* scales;   // of the workgroup's first row
+  uint32_t sat, step, most;  // this lane's row of the first tile in them, from tile to tile, the last row
 
   static constexpr int NV = WAVE / 4;
   __device__ static __forceinline__ int swizzle(int i) { return B ? (i & 3) | (i / (NV / 4) & 4) : i & 7; }
@@ -97,26 +97,25 @@ struct Slab8 {
       : base(q + o * ld),
         scales(s + o * (ld / kBlock8)) {
     const int64_t left = rows - o;  // rows behind the last read that one, for products that are not stored
-#pragma unroll
-    for (int j = 0; j < L; ++j) {
-      const int u = tid + NT * j, r = u / CH, c = (u % CH) ^ swizzle(r);
-      at[j] = (uint32_t)min((int64_t)r, left - 1) * (uint32_t)ld + 16 * c;
-    }
+    // (the rows of a lane's loads are NT / CH apart, which the swizzle does not see)
+    const int r0 = tid / CH, c = (tid % CH) ^ swizzle(r0);
+    at = (uint32_t)r0 * (uint32_t)ld + 16 * c;
+    last = (uint32_t)min(left - 1, (int64_t)W) * (uint32_t)ld + 16 * c;
+    far = NT / CH * (uint32_t)ld;
     const int lane = tid & 63, l16 = lane & 15, gq = lane >> 4;
     const int r = WAVE * wave + (B ? NV * (l16 >> 2) + (l16 & 3) : l16);
 #pragma unroll
     for (int h = 0; h < 2; ++h) v[h] = 16 * (r * CH + ((WIDE ? 2 * gq + h : 4 * h + gq) ^ swizzle(r)));
-#pragma unroll
-    for (int t = 0; t < WAVE / 16; ++t) {
-      const int64_t row = r + (B ? 4 : 16) * t;
-      sat[t] = (uint32_t)min(row, left - 1) * (uint32_t)(ld / kBlock8);
-    }
+    const uint32_t sld = (uint32_t)(ld / kBlock8);
+    sat = r * sld;
+    step = (B ? 4 : 16) * sld;
+    most = (uint32_t)min(left - 1, (int64_t)W) * sld;
   }
   // the loads of the whole stage from k on; d: the slab + 64 * wave
   __device__ __forceinline__ void issue(uint4* d, int64_t k) const {
     const char* s = reinterpret_cast<const char*>(base) + k;
 #pragma unroll
-    for (int j = 0; j < L; ++j) lds_load16(s + at[j], d + NT * j);
+    for (int j = 0; j < L; ++j) lds_load16(s + min(at + j * far, last), d + NT * j);
   }
   // the last `left` k's, fewer than a stage, and zeros
   __device__ __forceinline__ void issue_rest(uint4* d, int64_t k, int left, int tid) const {
@@ -124,7 +123,7 @@ struct Slab8 {
 #pragma unroll
     for (int j = 0; j < L; ++j) {
       const int u = tid + NT * j;
-      if (16 * ((u % CH) ^ swizzle(u / CH)) < left) lds_load16(s + at[j], d + NT * j);
+      if (16 * ((u % CH) ^ swizzle(u / CH)) < left) lds_load16(s + min(at + j * far, last), d + NT * j);
       else d[NT * j + (tid & 63)] = make_uint4(0, 0, 0, 0);
     }
   }
@@ -136,18 +135,20 @@ struct Slab8 {
     o.u[1] = *reinterpret_cast<const uint4*>(p + v[1]);
     return o;
   }
+  // tile t's row of scales; rows behind the last read that one
+  __device__ __forceinline__ uint32_t row_of(int t) const { return min(sat + t * step, most); }
   // tile t's scale byte for the stage at k, of which only `left` k's are there; any power for the blocks behind
   // them, where all values are 0
   __device__ __forceinline__ int rest_scale(int64_t k, int t, int gq, int left) const {
     const bool there = 32 * gq < left;
-    const int v = scales[sat[t] + (there ? gq : 0) + (uint32_t)(k / kBlock8)];
+    const int v = scales[row_of(t) + (there ? gq : 0) + (uint32_t)(k / kBlock8)];
     return there ? v : 127;
   }
   // tile t's scale bytes of four stages from k on in one load: lane group gq gets the four blocks of stage gq (of
   // `stages` that are there: of the last one else)
   __device__ __forceinline__ uint32_t four_scales(int64_t k, int t, int gq, int stages) const {
     uint32_t w;
-    __builtin_memcpy(&w, scales + sat[t] + (uint32_t)(k / kBlock8) + 4 * min(gq, stages - 1), 4);
+    __builtin_memcpy(&w, scales + row_of(t) + (uint32_t)(k / kBlock8) + 4 * min(gq, stages - 1), 4);
     return w;
   }
 };
@@ -161,9 +162,10 @@ __device__ __forceinline__ uint32_t turn_scales(uint32_t w, uint32_t sel) {
                                0x05040100u);
 }
 
-// NV (8 or 16) neighbouring values of row m from column n on, in eight bits; JOIN, the lanes of a block: all lanes of
-// the wave together.  there: the row exists (columns behind the last are not stored).
-enum { kNeighbours, kRowsApart };
+// NV (8 or 16) neighbouring values of row m from column n on, in eight bits; JOIN, which lanes have the rest of the
+// block: the next ones, the ones 16 apart, the one 32 apart.  All lanes of the wave together.  there: the row exists
+// (columns behind the last are not stored).
+enum { kNeighbours, kRowsApart, kHalves };
 template <int NV, int JOIN>
 __device__ __forceinline__ void store8(const Rows8& o, int64_t m, int64_t n, int64_t N, const float (&z)[NV],
                                        bool there) {
@@ -175,16 +177,15 @@ __device__ __forceinline__ void store8(const Rows8& o, int64_t m, int64_t n, int
     for (int i = 0; i < NV; ++i) v[i] = n + i < N ? z[i] : 0.f;
   }
   constexpr int LANES = kBlock8 / NV;
-  const int byte =
-      block_scale8(v, [](float top) { return JOIN == kNeighbours ? lanes_max<LANES>(top) : rows_max<LANES>(top); });
+  const int byte = block_scale8(v, [](float top) {
+    return JOIN == kNeighbours ? lanes_max<LANES>(top) : JOIN == kRowsApart ? rows_max<LANES>(top) : halves_max(top);
+  });
   uint32_t w[NV / 4];
   round8(v, byte, w);
   if (!there || n >= o.ld) return;
-  typedef uint32_t Words __attribute__((ext_vector_type(NV / 4)));
-  Words u;
-#pragma unroll
-  for (int i = 0; i < NV / 4; ++i) u[i] = w[i];
-  *reinterpret_cast<Words*>(o.q + m * o.ld + n) = u;
+  uint8_t* q = o.q + m * o.ld + n;
+  if constexpr (NV == 8) *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
+  else *reinterpret_cast<uint4*>(q) = make_uint4(w[0], w[1], w[2], w[3]);
   if (n % kBlock8 == 0) o.s[m * (o.ld / kBlock8) + n / kBlock8] = (uint8_t)byte;
 }
 
@@ -273,6 +274,28 @@ __device__ __forceinline__ bool whole_units8(const Mx8Args<T>& g) {
   return (uintptr_t)g.e.out % 16 == 0 && g.N % (16 / sizeof(T)) == 0;
 }
 
+// NV neighbouring sums of row m from column n on: a split's, or the results.  All lanes of the wave together.
+template <typename T, int NV, int JOIN>
+__device__ __forceinline__ void mx8_out(const Mx8Args<T>& g, const Drop& d, int64_t m, int64_t n, int split,
+                                        const float (&bias)[NV], float (&o)[NV], bool units) {
+  if (!g.part) {
+    finish8<T, NV, JOIN>(g, d, m, n, bias, o, units);
+    return;
+  }
+  if (m >= g.M) return;
+  float* p = g.part + (split * g.M + m) * g.N + n;
+  if (g.N % 4 == 0) {
+#pragma unroll
+    for (int i = 0; i < NV / 4; ++i)
+      if (n + 4 * i < g.N)
+        *reinterpret_cast<float4*>(p + 4 * i) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
+  } else {
+#pragma unroll
+    for (int e = 0; e < NV; ++e)
+      if (n + e < g.N) p[e] = o[e];
+  }
+}
+
 // The epilogue of a wave's TM x TN tiles without LDS: this lane has row l16 of every 16 and 4 TN neighbouring
 // columns.  m0, n0: the wave's first row and column.
 template <typename T, int TM, int TN>
@@ -292,22 +315,7 @@ __device__ __forceinline__ void mx8_store(const Mx8Args<T>& g, const Drop& d, co
     float o[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) o[i] = acc[a][i / 4][i % 4];
-    if (!g.part) {
-      finish8<T, NV, kRowsApart>(g, d, m, n, bias, o, units);
-      continue;
-    }
-    if (m >= g.M) continue;
-    float* p = g.part + (split * g.M + m) * g.N + n;
-    if (g.N % 4 == 0) {
-#pragma unroll
-      for (int i = 0; i < TN; ++i)
-        if (n + 4 * i < g.N)
-          *reinterpret_cast<float4*>(p + 4 * i) = make_float4(o[4 * i], o[4 * i + 1], o[4 * i + 2], o[4 * i + 3]);
-    } else {
-#pragma unroll
-      for (int e = 0; e < NV; ++e)
-        if (n + e < g.N) p[e] = o[e];
-    }
+    mx8_out<T, NV, kRowsApart>(g, d, m, n, split, bias, o, units);
   }
 }
 
@@ -450,6 +458,143 @@ __global__ void __launch_bounds__(256) mx8_gemm_tile(Mx8Args<T> g) {
     products(rest, ca, cb);
   }
   mx8_store<T, TM, TN>(g, d, acc, m0 + WR * wm, n0 + WR * wn, t.split, lane);
+}
+
+// a row's first scale bytes, up to 16; any power behind them
+__device__ __forceinline__ uint4 row_scales(const uint8_t* p, int blocks) {
+  union { uint4 u; uint8_t b[16]; } w;
+  if (blocks >= 16) {
+    __builtin_memcpy(&w.u, p, 16);
+  } else {
+    w.u = make_uint4(0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu);
+#pragma unroll
+    for (int i = 0; i < 15; ++i)
+      if (i < blocks) w.b[i] = p[i];
+  }
+  return w.u;
+}
+
+// Workgroup tile 256 x 256 in bf16, 8 waves as 2 x 4 of 128 x 64, two LDS buffers of 64 KB, the two groups of waves
+// in turn at the LDS and the matrix cores as in gemm_tile256: a stage is four turns of two row tiles by four column tiles.
+// The scales of four stages lie in the LDS, 16 bytes to a row, which each thread loads for one row (in registers
+// they spill).
+__global__ void __launch_bounds__(512) mx8_gemm_tile256(Mx8Args<bf16> g) {
+  constexpr int BK = 128, TM = 8, TN = 4;
+  typedef Slab8<false, false, 256, 128, 512> SA;
+  typedef Slab8<true, false, 256, 64, 512> SB;
+  __shared__ uint4 st0[SA::U + SB::U];
+  __shared__ uint4 st1[SA::U + SB::U];
+  __shared__ uint4 scales[2][512];
+  const TilePlace t((g.M + 255) / 256, (g.N + 255) / 256, g.splits);
+  if (!t.any) return;
+  const int64_t m0 = t.m * 256, n0 = t.n * 256;
+  const int64_t k0 = t.split * g.kper, k1 = min(g.ld, k0 + g.kper);
+  const int tid = threadIdx.x, lane = tid & 63, gq = lane >> 4, l16 = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 2, wn = wave & 3;
+  const int S = (int)((k1 - k0) / BK), left = (int)(k1 - k0 - (int64_t)S * BK);  // whole stages, the rest
+  const SA sa(g.a, g.as, g.ld, m0, g.M, tid, wm);
+  const SB sb(g.b, g.bs, g.ld, n0, g.N, tid, wn);
+  // the row whose scales this thread loads: of a, then of b.  The last four stages' 16 bytes are the last 16 of the
+  // split's, with those of fewer stages behind `shift` earlier ones.
+  const int64_t sld = g.ld / kBlock8;
+  const int blocks = (int)((k1 - k0) / kBlock8);
+  const uint8_t* row = (tid < 256 ? g.as + min(m0 + tid, g.M - 1) * sld : g.bs + min(n0 + tid - 256, g.N - 1) * sld) +
+                       k0 / kBlock8;
+  // this wave's places in them
+  const int pa = 16 * (128 * wm + l16) + gq, pb = 16 * (256 + 64 * wn + SB::NV * (l16 >> 2) + (l16 & 3)) + gq;
+
+  f32x4 acc[TM][TN];
+#pragma unroll
+  for (int a = 0; a < TM; ++a)
+#pragma unroll
+    for (int b = 0; b < TN; ++b) acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  auto sync = [&]() {  // everything that this wave has under way, then every wave's
+    asm volatile("" ::: "memory");
+    __builtin_amdgcn_s_waitcnt(kWaitAll);
+    dma_barrier();
+  };
+  // a scale byte; any power for the blocks that a rest has not, where all values are 0
+  auto scale = [&](const uint8_t* p, auto rest) { return decltype(rest)::value && 32 * gq >= left ? 127 : (int)*p; };
+  const std::integral_constant<bool, false> whole;
+  Mx8Op fa[2], fb[TN];
+  int cb[TN];
+  uint4 next_scales;
+  // stage `first` + j, first a multiple of four, from st, the next one into `next`; rest: it has `left` k's alone
+  auto stage = [&](const uint4* st, uint4* next, int first, int j, auto rest) {
+    const int shift = first ? 4 * first - min(4 * first, blocks - 16) : 0;
+    const uint8_t* sc = reinterpret_cast<const uint8_t*>(scales[first >> 2 & 1]) + shift + 4 * j;
+    const int64_t kn = k0 + (int64_t)min(first + j + 1, S - 1) * BK;  // behind the last: that again, nobody reads it
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      if (q == 0) {
+#pragma unroll
+        for (int b = 0; b < TN; ++b) fb[b] = sb.read(st + SA::U, b);
+#pragma unroll
+        for (int b = 0; b < TN; ++b) cb[b] = scale(sc + pb + 16 * 4 * b, rest);
+      }
+      int ca[2];
+#pragma unroll
+      for (int a = 0; a < 2; ++a) fa[a] = sa.read(st, 2 * q + a);
+#pragma unroll
+      for (int a = 0; a < 2; ++a) ca[a] = scale(sc + pa + 16 * 16 * (2 * q + a), rest);
+      if (next && q == 0) sa.issue(next + 64 * wave, kn);
+      if (next && q == 1) sb.issue(next + SA::U + 64 * wave, kn);
+      __builtin_amdgcn_sched_barrier(0);
+      __builtin_amdgcn_s_waitcnt(kWaitLds);
+      if (q == 3) __builtin_amdgcn_s_waitcnt(kWaitAll);
+      dma_barrier();
+      __builtin_amdgcn_s_setprio(1);
+      mx8_products<bf16>(fa, fb, ca, cb, acc, 2 * q);
+      // the products stay in their turn: the compiler moves them over barriers, and then has too few registers
+      asm volatile("" : "+v"(acc[2 * q][0]), "+v"(acc[2 * q][1]), "+v"(acc[2 * q][2]), "+v"(acc[2 * q][3]),
+                   "+v"(acc[2 * q + 1][0]), "+v"(acc[2 * q + 1][1]), "+v"(acc[2 * q + 1][2]), "+v"(acc[2 * q + 1][3]));
+      __builtin_amdgcn_s_setprio(0);
+      dma_barrier();
+    }
+  };
+  // every wave passes the same number of barriers: the second group one more ahead, the first behind
+  next_scales = row_scales(row, blocks);
+  if (S) {
+    sa.issue(st0 + 64 * wave, k0);
+    sb.issue(st0 + SA::U + 64 * wave, k0);
+  }
+  scales[0][tid] = next_scales;
+  const Drop d(g.e.drop);  // its load of the counter under cover of the first stage's
+  if (S) {
+    sync();
+    if (wave >= 4) dma_barrier();
+    int s = 0;
+    // no way out or branch inside the loop: with one, the accumulators live in two sets of registers
+    for (; s + 3 < S; s += 4) {
+      __builtin_memcpy(&next_scales, row + min(4 * s + 16, blocks - 16), 16);
+      stage(st0, st1, s, 0, whole);
+      stage(st1, st0, s, 1, whole);
+      scales[(s >> 2 & 1) ^ 1][tid] = next_scales;
+      stage(st0, st1, s, 2, whole);
+      stage(st1, st0, s, 3, whole);
+    }
+    if (S & 2) {
+      stage(st0, st1, s, 0, whole);
+      stage(st1, st0, s, 1, whole);
+    }
+    if (S & 1) stage(st0, nullptr, s, S & 2, whole);
+    if (wave < 4) dma_barrier();
+  }
+  if (left > 0) {
+    const int64_t k = k0 + (int64_t)S * BK;
+    sync();
+    sa.issue_rest(st0 + 64 * wave, k, left, tid);
+    sb.issue_rest(st0 + SA::U + 64 * wave, k, left, tid);
+    sync();
+    if (wave >= 4) dma_barrier();
+    stage(st0, nullptr, S & ~3, S & 3, std::integral_constant<bool, true>());
+    if (wave < 4) dma_barrier();
+  }
+  // the surplus loads land before the workgroup's LDS can pass to another
+  asm volatile("" ::: "memory");
+  __builtin_amdgcn_s_waitcnt(wait_loads(0));
+  asm volatile("" ::: "memory");
+  mx8_store<bf16, TM, TN>(g, d, acc, m0 + 128 * wm, n0 + 64 * wn, t.split, lane);
 }
 
 // The splits' sums added in order, then the epilogue; eight neighbouring elements a thread, four threads a block.

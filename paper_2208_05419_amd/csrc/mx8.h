@@ -107,16 +107,17 @@ __device__ __forceinline__ float lanes_max(float v) {
   if constexpr (N >= 32) v = fmaxf(v, __shfl_xor(v, 16, 64));
   return v;
 }
+// the largest over lanes l and l + 32
+__device__ __forceinline__ float halves_max(float v) {
+  const auto a = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  return fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
+}
 // the largest over N lanes 16 apart: l and l + 16 of every 32, or l, l + 16, l + 32 and l + 48
 template <int N>
 __device__ __forceinline__ float rows_max(float v) {
   const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
   v = fmaxf(__uint_as_float(a[0]), __uint_as_float(a[1]));
-  if constexpr (N == 4) {
-    const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(v), __float_as_uint(v), false, false);
-    v = fmaxf(__uint_as_float(b[0]), __uint_as_float(b[1]));
-  }
-  return v;
+  return N == 4 ? halves_max(v) : v;
 }
 
 // The scale byte of a block whose values lie in several lanes, N in each, JOIN the largest over them: all lanes of

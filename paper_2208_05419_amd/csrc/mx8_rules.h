@@ -6,8 +6,9 @@
 namespace afno {
 
 // ld: bytes of a row, K rounded up to 32
-inline Cut cut_mx8(int64_t M, int64_t N, int64_t ld) {
+inline Cut cut_mx8(int64_t M, int64_t N, int64_t ld, int es) {
   Cut c;
+  if (es == 2 && ceil_div(M, 256) * ceil_div(N, 256) >= 128) return {256, 1, ceil_div(ld, 128) * 128};
   auto tiles = [&](int t) { return ceil_div(M, t) * ceil_div(N, t); };
   auto cut = [&](int tile, int64_t s) {
     c.tile = tile;
@@ -19,6 +20,8 @@ inline Cut cut_mx8(int64_t M, int64_t N, int64_t ld) {
   const int64_t t = tiles(64);
   return cut(64, t >= 256 ? 1 : std::max<int64_t>(1, std::min<int64_t>(256 / t, ld / 1024)));
 }
-inline size_t mx8_part_bytes(int64_t M, int64_t N, int64_t ld) { return part_of(M, N, cut_mx8(M, N, ld)); }
+inline size_t mx8_part_bytes(int64_t M, int64_t N, int64_t ld, int es) {
+  return part_of(M, N, cut_mx8(M, N, ld, es));
+}
 
 }  // namespace afno
