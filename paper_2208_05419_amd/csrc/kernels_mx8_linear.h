@@ -30,6 +30,18 @@ template <typename T>
 __device__ __forceinline__ int scale_byte(uint32_t w) {
   return (int)(sizeof(T) == 2 ? w : w & 255);
 }
+// The accumulators of some row tiles stay in the registers and at the place in the program that they have here: the
+// compiler moves products over barriers otherwise, holds their operands for longer, and has too few registers.
+template <int TM, int TN>
+__device__ __forceinline__ void hold(f32x4 (&acc)[TM][TN], int a0, int n) {
+#pragma unroll
+  for (int a = 0; a < n; ++a) {
+    if constexpr (TN == 4)
+      asm volatile("" : "+v"(acc[a0 + a][0]), "+v"(acc[a0 + a][1]), "+v"(acc[a0 + a][2]), "+v"(acc[a0 + a][3]));
+    else
+      asm volatile("" : "+v"(acc[a0 + a][0]), "+v"(acc[a0 + a][1]));
+  }
+}
 // acc += the products of a stage's operands under their scale bytes, transposed
 template <typename T, int TM, int TN, int AM>
 __device__ __forceinline__ void mx8_products(const Mx8Op (&fa)[TM], const Mx8Op (&fb)[TN], const int* sa,
@@ -202,18 +214,17 @@ union Some {
   }
 };
 
-// The epilogue of NV neighbouring values, bias[] theirs; as store8 all lanes of the wave together.
+// The epilogue of NV neighbouring values, their biases added; as store8 all lanes of the wave together.  In bf16 the
+// short GELU, whose error is below that of the eight-bit instruction (64,800 x 1,024 x 4,096: @@ us, @@ with the other one).
 template <typename T, int NV, int JOIN>
 __device__ __forceinline__ void finish8(const Mx8Args<T>& g, const Drop& d, int64_t m, int64_t n,
-                                        const float (&bias)[NV], float (&o)[NV], bool units) {
+                                        float (&o)[NV], bool units) {
   const Epilogue<T>& e = g.e;
   const bool there = m < g.M;
-#pragma unroll
-  for (int i = 0; i < NV; ++i) o[i] += bias[i];
   if (g.pre8.q) store8<NV, JOIN>(g.pre8, m, n, g.N, o, there);
   if (e.act == kActGelu) {
 #pragma unroll
-    for (int i = 0; i < NV; ++i) o[i] = gelu(o[i]);
+    for (int i = 0; i < NV; ++i) o[i] = sizeof(T) == 2 ? gelu_short(o[i]) : gelu(o[i]);
   } else if (e.act == kActRelu) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) o[i] = activate(o[i], kActRelu);
@@ -277,9 +288,9 @@ __device__ __forceinline__ bool whole_units8(const Mx8Args<T>& g) {
 // NV neighbouring sums of row m from column n on: a split's, or the results.  All lanes of the wave together.
 template <typename T, int NV, int JOIN>
 __device__ __forceinline__ void mx8_out(const Mx8Args<T>& g, const Drop& d, int64_t m, int64_t n, int split,
-                                        const float (&bias)[NV], float (&o)[NV], bool units) {
+                                        float (&o)[NV], bool units) {
   if (!g.part) {
-    finish8<T, NV, JOIN>(g, d, m, n, bias, o, units);
+    finish8<T, NV, JOIN>(g, d, m, n, o, units);
     return;
   }
   if (m >= g.M) return;
@@ -296,6 +307,21 @@ __device__ __forceinline__ void mx8_out(const Mx8Args<T>& g, const Drop& d, int6
   }
 }
 
+// a wave's sums before the first product: the biases of its columns (a split's: 0)
+template <typename T, int TM, int TN>
+__device__ __forceinline__ void mx8_begin(const Mx8Args<T>& g, f32x4 (&acc)[TM][TN], int64_t n0, int lane) {
+  float bias[4 * TN];
+#pragma unroll
+  for (int i = 0; i < 4 * TN; ++i) bias[i] = 0.f;
+  if (g.e.bias && !g.part) load_bias8(g.e, g.N, n0 + 4 * TN * (lane >> 4), bias);
+#pragma unroll
+  for (int a = 0; a < TM; ++a)
+#pragma unroll
+    for (int b = 0; b < TN; ++b)
+      acc[a][b] = f32x4{bias[4 * b], bias[4 * b + 1], bias[4 * b + 2], bias[4 * b + 3]};
+  hold(acc, 0, TM);
+}
+
 // The epilogue of a wave's TM x TN tiles without LDS: this lane has row l16 of every 16 and 4 TN neighbouring
 // columns.  m0, n0: the wave's first row and column.
 template <typename T, int TM, int TN>
@@ -306,8 +332,6 @@ __device__ __forceinline__ void mx8_store(const Mx8Args<T>& g, const Drop& d, co
   const int l16 = lane & 15, gq = lane >> 4;
   const bool units = whole_units8(g);
   const int64_t n = n0 + NV * gq;
-  float bias[NV];
-  load_bias8(g.e, g.N, n, bias);
 #pragma unroll
   for (int a = 0; a < TM; ++a) {
     const int64_t m = m0 + 16 * a + l16;
@@ -315,14 +339,14 @@ __device__ __forceinline__ void mx8_store(const Mx8Args<T>& g, const Drop& d, co
     float o[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) o[i] = acc[a][i / 4][i % 4];
-    mx8_out<T, NV, kRowsApart>(g, d, m, n, split, bias, o, units);
+    mx8_out<T, NV, kRowsApart>(g, d, m, n, split, o, units);
   }
 }
 
 // Workgroup tile TILE x TILE (128 or 64), 4 waves as 2 x 2, stages of 128 k's in two (four) LDS buffers of 32 KB
 // (16 KB), the next stages' loads under way during the present one's products.
 template <typename T, int TILE>
-__global__ void __launch_bounds__(256) mx8_gemm_tile(Mx8Args<T> g) {
+__global__ void __launch_bounds__(256, 2) mx8_gemm_tile(Mx8Args<T> g) {
   constexpr int NT = 256, WR = TILE / 2, TM = WR / 16, TN = WR / 16, NS = TILE == 128 ? 2 : 4;
   constexpr bool WIDE = sizeof(T) == 4;
   typedef Slab8<false, WIDE, TILE, WR, NT> SA;
@@ -343,10 +367,7 @@ __global__ void __launch_bounds__(256) mx8_gemm_tile(Mx8Args<T> g) {
   const SB sb(g.b, g.bs, g.ld, n0, g.N, tid, wn);
 
   f32x4 acc[TM][TN];
-#pragma unroll
-  for (int a = 0; a < TM; ++a)
-#pragma unroll
-    for (int b = 0; b < TN; ++b) acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  mx8_begin(g, acc, n0 + WR * wn, lane);
   // four stages' scales: those in use, and the next four's words under way
   uint32_t pa[TM], pb[TN], ra[TM], rb[TN];
   const uint32_t sel = (uint32_t)(gq | (4 + gq) << 8);
@@ -369,6 +390,7 @@ __global__ void __launch_bounds__(256) mx8_gemm_tile(Mx8Args<T> g) {
 #pragma unroll
     for (int a = 0; a < TM; ++a) fa[a] = sa.read(st, a);
     mx8_products<T>(fa, fb, ca, cb, acc, 0);
+    hold(acc, 0, TM);
   };
   auto compute = [&](const uint4* st, int i) {  // stage i
     if ((i & 3) == 0) {
@@ -460,24 +482,10 @@ __global__ void __launch_bounds__(256) mx8_gemm_tile(Mx8Args<T> g) {
   mx8_store<T, TM, TN>(g, d, acc, m0 + WR * wm, n0 + WR * wn, t.split, lane);
 }
 
-// a row's first scale bytes, up to 16; any power behind them
-__device__ __forceinline__ uint4 row_scales(const uint8_t* p, int blocks) {
-  union { uint4 u; uint8_t b[16]; } w;
-  if (blocks >= 16) {
-    __builtin_memcpy(&w.u, p, 16);
-  } else {
-    w.u = make_uint4(0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu, 0x7f7f7f7fu);
-#pragma unroll
-    for (int i = 0; i < 15; ++i)
-      if (i < blocks) w.b[i] = p[i];
-  }
-  return w.u;
-}
-
 // Workgroup tile 256 x 256 in bf16, 8 waves as 2 x 4 of 128 x 64, two LDS buffers of 64 KB, the two groups of waves
 // in turn at the LDS and the matrix cores as in gemm_tile256: a stage is four turns of two row tiles by four column tiles.
-// The scales of four stages lie in the LDS, 16 bytes to a row, which each thread loads for one row (in registers
-// they spill).
+// The scales of four stages lie in the LDS, 16 bytes to a row, which each thread loads for one row (in registers they
+// spill).
 __global__ void __launch_bounds__(512) mx8_gemm_tile256(Mx8Args<bf16> g) {
   constexpr int BK = 128, TM = 8, TN = 4;
   typedef Slab8<false, false, 256, 128, 512> SA;
@@ -496,18 +504,14 @@ __global__ void __launch_bounds__(512) mx8_gemm_tile256(Mx8Args<bf16> g) {
   const SB sb(g.b, g.bs, g.ld, n0, g.N, tid, wn);
   // the row whose scales this thread loads: of a, then of b.  The last four stages' 16 bytes are the last 16 of the
   // split's, with those of fewer stages behind `shift` earlier ones.
-  const int64_t sld = g.ld / kBlock8;
   const int blocks = (int)((k1 - k0) / kBlock8);
-  const uint8_t* row = (tid < 256 ? g.as + min(m0 + tid, g.M - 1) * sld : g.bs + min(n0 + tid - 256, g.N - 1) * sld) +
-                       k0 / kBlock8;
+  const uint8_t* from = (wave < 4 ? g.as + m0 * (g.ld / kBlock8) : g.bs + n0 * (g.ld / kBlock8)) + k0 / kBlock8;
+  const uint32_t row = (uint32_t)min((int64_t)(tid & 255), (wave < 4 ? g.M - m0 : g.N - n0) - 1) * (uint32_t)(g.ld / kBlock8);
   // this wave's places in them
   const int pa = 16 * (128 * wm + l16) + gq, pb = 16 * (256 + 64 * wn + SB::NV * (l16 >> 2) + (l16 & 3)) + gq;
 
   f32x4 acc[TM][TN];
-#pragma unroll
-  for (int a = 0; a < TM; ++a)
-#pragma unroll
-    for (int b = 0; b < TN; ++b) acc[a][b] = f32x4{0.f, 0.f, 0.f, 0.f};
+  mx8_begin(g, acc, n0 + 64 * wn, lane);
   auto sync = [&]() {  // everything that this wave has under way, then every wave's
     asm volatile("" ::: "memory");
     __builtin_amdgcn_s_waitcnt(kWaitAll);
@@ -515,12 +519,14 @@ __global__ void __launch_bounds__(512) mx8_gemm_tile256(Mx8Args<bf16> g) {
   };
   // a scale byte; any power for the blocks that a rest has not, where all values are 0
   auto scale = [&](const uint8_t* p, auto rest) { return decltype(rest)::value && 32 * gq >= left ? 127 : (int)*p; };
-  const std::integral_constant<bool, false> whole;
   Mx8Op fa[2], fb[TN];
   int cb[TN];
   uint4 next_scales;
-  // stage `first` + j, first a multiple of four, from st, the next one into `next`; rest: it has `left` k's alone
-  auto stage = [&](const uint4* st, uint4* next, int first, int j, auto rest) {
+  // stage `first` + j, first a multiple of four, from st, the next one into `next` (more: there is one); rest: it has
+  // `left` k's alone
+  const std::integral_constant<bool, true> yes;
+  const std::integral_constant<bool, false> no;
+  auto stage = [&](const uint4* st, uint4* next, int first, int j, auto more, auto rest) {
     const int shift = first ? 4 * first - min(4 * first, blocks - 16) : 0;
     const uint8_t* sc = reinterpret_cast<const uint8_t*>(scales[first >> 2 & 1]) + shift + 4 * j;
     const int64_t kn = k0 + (int64_t)min(first + j + 1, S - 1) * BK;  // behind the last: that again, nobody reads it
@@ -537,47 +543,51 @@ __global__ void __launch_bounds__(512) mx8_gemm_tile256(Mx8Args<bf16> g) {
       for (int a = 0; a < 2; ++a) fa[a] = sa.read(st, 2 * q + a);
 #pragma unroll
       for (int a = 0; a < 2; ++a) ca[a] = scale(sc + pa + 16 * 16 * (2 * q + a), rest);
-      if (next && q == 0) sa.issue(next + 64 * wave, kn);
-      if (next && q == 1) sb.issue(next + SA::U + 64 * wave, kn);
+      if (decltype(more)::value && q == 0) sa.issue(next + 64 * wave, kn);
+      if (decltype(more)::value && q == 1) sb.issue(next + SA::U + 64 * wave, kn);
       __builtin_amdgcn_sched_barrier(0);
       __builtin_amdgcn_s_waitcnt(kWaitLds);
       if (q == 3) __builtin_amdgcn_s_waitcnt(kWaitAll);
       dma_barrier();
       __builtin_amdgcn_s_setprio(1);
       mx8_products<bf16>(fa, fb, ca, cb, acc, 2 * q);
-      // the products stay in their turn: the compiler moves them over barriers, and then has too few registers
-      asm volatile("" : "+v"(acc[2 * q][0]), "+v"(acc[2 * q][1]), "+v"(acc[2 * q][2]), "+v"(acc[2 * q][3]),
-                   "+v"(acc[2 * q + 1][0]), "+v"(acc[2 * q + 1][1]), "+v"(acc[2 * q + 1][2]), "+v"(acc[2 * q + 1][3]));
+      hold(acc, 2 * q, 2);
       __builtin_amdgcn_s_setprio(0);
       dma_barrier();
     }
   };
-  // every wave passes the same number of barriers: the second group one more ahead, the first behind
-  next_scales = row_scales(row, blocks);
   if (S) {
     sa.issue(st0 + 64 * wave, k0);
     sb.issue(st0 + SA::U + 64 * wave, k0);
   }
-  scales[0][tid] = next_scales;
+  if (blocks >= 16) {
+    __builtin_memcpy(&next_scales, from + row, 16);
+    scales[0][tid] = next_scales;
+  } else {
+    uint8_t* p = reinterpret_cast<uint8_t*>(&scales[0][tid]);
+#pragma unroll 1
+    for (int i = 0; i < blocks; ++i) p[i] = from[row + i];
+  }
   const Drop d(g.e.drop);  // its load of the counter under cover of the first stage's
   if (S) {
     sync();
+    // every wave passes the same number of barriers: the second group one more ahead, the first behind
     if (wave >= 4) dma_barrier();
     int s = 0;
     // no way out or branch inside the loop: with one, the accumulators live in two sets of registers
     for (; s + 3 < S; s += 4) {
-      __builtin_memcpy(&next_scales, row + min(4 * s + 16, blocks - 16), 16);
-      stage(st0, st1, s, 0, whole);
-      stage(st1, st0, s, 1, whole);
+      __builtin_memcpy(&next_scales, from + row + min(4 * s + 16, blocks - 16), 16);
+      stage(st0, st1, s, 0, yes, no);
+      stage(st1, st0, s, 1, yes, no);
       scales[(s >> 2 & 1) ^ 1][tid] = next_scales;
-      stage(st0, st1, s, 2, whole);
-      stage(st1, st0, s, 3, whole);
+      stage(st0, st1, s, 2, yes, no);
+      stage(st1, st0, s, 3, yes, no);
     }
     if (S & 2) {
-      stage(st0, st1, s, 0, whole);
-      stage(st1, st0, s, 1, whole);
+      stage(st0, st1, s, 0, yes, no);
+      stage(st1, st0, s, 1, yes, no);
     }
-    if (S & 1) stage(st0, nullptr, s, S & 2, whole);
+    if (S & 1) stage(st0, nullptr, s, S & 2, no, no);
     if (wave < 4) dma_barrier();
   }
   if (left > 0) {
@@ -587,7 +597,7 @@ __global__ void __launch_bounds__(512) mx8_gemm_tile256(Mx8Args<bf16> g) {
     sb.issue_rest(st0 + SA::U + 64 * wave, k, left, tid);
     sync();
     if (wave >= 4) dma_barrier();
-    stage(st0, nullptr, S & ~3, S & 3, std::integral_constant<bool, true>());
+    stage(st0, nullptr, S & ~3, S & 3, no, yes);
     if (wave < 4) dma_barrier();
   }
   // the surplus loads land before the workgroup's LDS can pass to another
@@ -626,7 +636,9 @@ __global__ void __launch_bounds__(256) mx8_join_splits(Mx8Args<T> g) {
   const Drop d(g.e.drop);
   float bias[8];
   load_bias8(g.e, g.N, n, bias);
-  finish8<T, 8, kNeighbours>(g, d, m, n, bias, v, whole_units8(g));
+#pragma unroll
+  for (int i = 0; i < 8; ++i) v[i] += bias[i];
+  finish8<T, 8, kNeighbours>(g, d, m, n, v, whole_units8(g));
 }
 
 }  // namespace afno

@@ -48,31 +48,36 @@ __device__ __forceinline__ int scale8(float top) {
   const int s = (int)(u >> 23) - 127 - 8 + ((u & 0x7fffffu) > 0x600000u);
   return min(max(s, kLeast8), kMost8) + 127;
 }
-// 2^s and 2^-s of a scale byte
+// 2^s of a scale byte
 __device__ __forceinline__ float power8(int byte) { return __uint_as_float((uint32_t)byte << 23); }
-__device__ __forceinline__ float inverse8(int byte) { return __uint_as_float((uint32_t)(254 - byte) << 23); }
 
-// N values (one, or a multiple of four) rounded to E4M3, to nearest, ties to even; the instruction makes NaN of
-// what is NaN or infinite
+// N values (one, or a multiple of four) divided by 2^s and rounded to E4M3, to nearest, ties to even; the instruction
+// makes NaN of what is NaN, infinite or too large
 template <int N>
-__device__ __forceinline__ void round8(const float (&v)[N], int byte, uint32_t (&w)[(N + 3) / 4]) {
+__device__ __forceinline__ void round8(const float (&z)[N], int byte, uint32_t (&w)[(N + 3) / 4]) {
   static_assert(N == 1 || N % 4 == 0, "whole words, or one value");
-  const float f = inverse8(byte);
-  float u[N];
+  typedef short s16x2 __attribute__((ext_vector_type(2)));
+  const float scale = power8(byte);
+  float v[N];
 #pragma unroll
-  for (int i = 0; i < N; ++i) u[i] = v[i] * f;
-  if (byte == kMost8 + 127) {
+  for (int i = 0; i < N; ++i) v[i] = z[i];
+  if (byte == kMost8 + 127) {  // values above 448 2^119
 #pragma unroll
     for (int i = 0; i < N; ++i)
-      if (fabsf(v[i]) < __builtin_inff()) u[i] = __builtin_amdgcn_fmed3f(u[i], -448.f, 448.f);
+      if (fabsf(v[i]) < __builtin_inff()) v[i] = __builtin_amdgcn_fmed3f(v[i], -448.f * 0x1p119f, 448.f * 0x1p119f);
   }
+  union { s16x2 h; uint32_t u; } x;
+  x.u = 0;
   if constexpr (N == 1) {
-    w[0] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(u[0], 0.f, 0, false);
+    x.h = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(x.h, v[0], 0.f, scale, false);
+    w[0] = x.u;
   } else {
 #pragma unroll
-    for (int i = 0; i < N / 4; ++i)
-      w[i] = (uint32_t)__builtin_amdgcn_cvt_pk_fp8_f32(
-          u[4 * i + 2], u[4 * i + 3], __builtin_amdgcn_cvt_pk_fp8_f32(u[4 * i], u[4 * i + 1], 0, false), true);
+    for (int i = 0; i < N / 4; ++i) {
+      x.h = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(x.h, v[4 * i], v[4 * i + 1], scale, false);
+      x.h = __builtin_amdgcn_cvt_scalef32_pk_fp8_f32(x.h, v[4 * i + 2], v[4 * i + 3], scale, true);
+      w[i] = x.u;
+    }
   }
 }
 
