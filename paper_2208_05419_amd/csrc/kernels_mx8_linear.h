@@ -96,7 +96,7 @@ template <bool B, bool WIDE, int W, int WAVE, int NT>
 struct Slab8 {
   static constexpr int CH = 8, U = W * CH, L = U / NT;  // chunks of a row, 16-byte units, loads a lane
   static_assert(U % NT == 0, "whole loads");
-  const uint8_t* base;  // the workgroup's first row
+  Buf base;  // the workgroup's rows
   uint32_t at, last, far;  // this lane's first load, bytes behind a stage's base, its place in the last row; from load to load
   int v[2];                // this lane's operand places, bytes into the slab
   const uint8_t* scales;   // of the workgroup's first row
@@ -106,8 +106,7 @@ struct Slab8 {
   __device__ static __forceinline__ int swizzle(int i) { return B ? (i & 3) | (i / (NV / 4) & 4) : i & 7; }
   __device__ __forceinline__ Slab8(const uint8_t* q, const uint8_t* s, int64_t ld, int64_t o, int64_t rows, int tid,
                                    int wave)
-      : base(q + o * ld),
-        scales(s + o * (ld / kBlock8)) {
+      : base(q + o * ld, (uint32_t)(min((int64_t)W, rows - o) * ld)), scales(s + o * (ld / kBlock8)) {
     const int64_t left = rows - o;  // rows behind the last read that one, for products that are not stored
     // (the rows of a lane's loads are NT / CH apart, which the swizzle does not see)
     const int r0 = tid / CH, c = (tid % CH) ^ swizzle(r0);
@@ -123,29 +122,39 @@ struct Slab8 {
     step = (B ? 4 : 16) * sld;
     most = (uint32_t)min(left - 1, (int64_t)W) * sld;
   }
+  // load j of the stage at k
+  __device__ __forceinline__ void load(uint4* d, int64_t k, int j) const {
+    __builtin_amdgcn_raw_ptr_buffer_load_lds(base.r, (__attribute__((address_space(3))) void*)(d + NT * j), 16,
+                                             (int)min(at + j * far, last), (int)k, 0, 0);
+  }
   // the loads of the whole stage from k on; d: the slab + 64 * wave
   __device__ __forceinline__ void issue(uint4* d, int64_t k) const {
-    const char* s = reinterpret_cast<const char*>(base) + k;
 #pragma unroll
-    for (int j = 0; j < L; ++j) lds_load16(s + min(at + j * far, last), d + NT * j);
+    for (int j = 0; j < L; ++j) load(d, k, j);
   }
   // the last `left` k's, fewer than a stage, and zeros
   __device__ __forceinline__ void issue_rest(uint4* d, int64_t k, int left, int tid) const {
-    const char* s = reinterpret_cast<const char*>(base) + k;
 #pragma unroll
     for (int j = 0; j < L; ++j) {
       const int u = tid + NT * j;
-      if (16 * ((u % CH) ^ swizzle(u / CH)) < left) lds_load16(s + min(at + j * far, last), d + NT * j);
+      if (16 * ((u % CH) ^ swizzle(u / CH)) < left) load(d, k, j);
       else d[NT * j + (tid & 63)] = make_uint4(0, 0, 0, 0);
     }
   }
-  // tile t's operand
-  __device__ __forceinline__ Mx8Op read(const uint4* slab, int t) const {
-    const char* p = reinterpret_cast<const char*>(slab) + (B ? 512 : 2048) * t;
-    Mx8Op o;
-    o.u[0] = *reinterpret_cast<const uint4*>(p + v[0]);
-    o.u[1] = *reinterpret_cast<const uint4*>(p + v[1]);
-    return o;
+  // A stage's operands: the places as they are in this stage alone (opq: one addition each, where the compiler otherwise
+  // keeps an address of its own for each tile and buffer in registers across the kernel).
+  struct Reader {
+    const char *p0, *p1;
+    __device__ __forceinline__ Mx8Op operator()(int t) const {
+      Mx8Op o;
+      o.u[0] = *reinterpret_cast<const uint4*>(p0 + (B ? 512 : 2048) * t);
+      o.u[1] = *reinterpret_cast<const uint4*>(p1 + (B ? 512 : 2048) * t);
+      return o;
+    }
+  };
+  __device__ __forceinline__ Reader read(const uint4* slab) const {
+    const char* p = reinterpret_cast<const char*>(slab);
+    return {p + opq(v[0]), p + opq(v[1])};
   }
   // tile t's row of scales; rows behind the last read that one
   __device__ __forceinline__ uint32_t row_of(int t) const { return min(sat + t * step, most); }
@@ -385,10 +394,12 @@ __global__ void __launch_bounds__(256, 2) mx8_gemm_tile(Mx8Args<T> g) {
   };
   auto products = [&](const uint4* st, const int (&ca)[TM], const int (&cb)[TN]) {
     Mx8Op fa[TM], fb[TN];
+    const auto rb = sb.read(st + SA::U);
+    const auto ra = sa.read(st);
 #pragma unroll
-    for (int b = 0; b < TN; ++b) fb[b] = sb.read(st + SA::U, b);
+    for (int b = 0; b < TN; ++b) fb[b] = rb(b);
 #pragma unroll
-    for (int a = 0; a < TM; ++a) fa[a] = sa.read(st, a);
+    for (int a = 0; a < TM; ++a) fa[a] = ra(a);
     mx8_products<T>(fa, fb, ca, cb, acc, 0);
     hold(acc, 0, TM);
   };
@@ -518,9 +529,11 @@ __global__ void __launch_bounds__(512) mx8_gemm_tile256(Mx8Args<bf16> g) {
     dma_barrier();
   };
   // a scale byte; any power for the blocks that a rest has not, where all values are 0
-  auto scale = [&](const uint8_t* p, auto rest) { return decltype(rest)::value && 32 * gq >= left ? 127 : (int)*p; };
+  auto scale = [&](int at, auto rest) {
+    const uint8_t v = reinterpret_cast<const uint8_t*>(scales)[at];
+    return decltype(rest)::value && 32 * gq >= left ? 127 : (int)v;
+  };
   Mx8Op fa[2], fb[TN];
-  int cb[TN];
   uint4 next_scales;
   // stage `first` + j, first a multiple of four, from st, the next one into `next` (more: there is one); rest: it has
   // `left` k's alone
@@ -528,21 +541,26 @@ __global__ void __launch_bounds__(512) mx8_gemm_tile256(Mx8Args<bf16> g) {
   const std::integral_constant<bool, false> no;
   auto stage = [&](const uint4* st, uint4* next, int first, int j, auto more, auto rest) {
     const int shift = first ? 4 * first - min(4 * first, blocks - 16) : 0;
-    const uint8_t* sc = reinterpret_cast<const uint8_t*>(scales[first >> 2 & 1]) + shift + 4 * j;
+    const int sc = 16 * 512 * (first >> 2 & 1) + shift + 4 * j;
     const int64_t kn = k0 + (int64_t)min(first + j + 1, S - 1) * BK;  // behind the last: that again, nobody reads it
+    const auto rb = sb.read(st + SA::U);
+    const auto ra = sa.read(st);
+    // all scales ahead of the loads into the LDS: the compiler waits for those before it reads an array that it does not
+    // see to be another one
+    int ca[TM], cb[TN];
+#pragma unroll
+    for (int b = 0; b < TN; ++b) cb[b] = scale(sc + pb + 16 * 4 * b, rest);
+#pragma unroll
+    for (int a = 0; a < TM; ++a) ca[a] = scale(sc + pa + 16 * 16 * a, rest);
 #pragma unroll
     for (int q = 0; q < 4; ++q) {
       if (q == 0) {
 #pragma unroll
-        for (int b = 0; b < TN; ++b) fb[b] = sb.read(st + SA::U, b);
-#pragma unroll
-        for (int b = 0; b < TN; ++b) cb[b] = scale(sc + pb + 16 * 4 * b, rest);
+        for (int b = 0; b < TN; ++b) fb[b] = rb(b);
       }
-      int ca[2];
 #pragma unroll
-      for (int a = 0; a < 2; ++a) fa[a] = sa.read(st, 2 * q + a);
-#pragma unroll
-      for (int a = 0; a < 2; ++a) ca[a] = scale(sc + pa + 16 * 16 * (2 * q + a), rest);
+      for (int a = 0; a < 2; ++a) fa[a] = ra(2 * q + a);
+      if (decltype(more)::value && q < 2) __builtin_amdgcn_sched_barrier(0);  // the reads first
       if (decltype(more)::value && q == 0) sa.issue(next + 64 * wave, kn);
       if (decltype(more)::value && q == 1) sb.issue(next + SA::U + 64 * wave, kn);
       __builtin_amdgcn_sched_barrier(0);
@@ -550,7 +568,7 @@ __global__ void __launch_bounds__(512) mx8_gemm_tile256(Mx8Args<bf16> g) {
       if (q == 3) __builtin_amdgcn_s_waitcnt(kWaitAll);
       dma_barrier();
       __builtin_amdgcn_s_setprio(1);
-      mx8_products<bf16>(fa, fb, ca, cb, acc, 2 * q);
+      mx8_products<bf16>(fa, fb, ca + 2 * q, cb, acc, 2 * q);
       hold(acc, 2 * q, 2);
       __builtin_amdgcn_s_setprio(0);
       dma_barrier();
