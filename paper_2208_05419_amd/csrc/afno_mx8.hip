@@ -122,7 +122,6 @@ size_t mx8_forward_bytes(const Mx8Fwd& a) { return mx8_part_bytes(a.M, a.N, a.x.
 hipError_t launch_mx8_forward(const Mx8Fwd& a, void* ws, hipStream_t st) {
   return by_type(a.dtype, [&](auto z) {
     typedef decltype(z) T;
-    const Cut c = cut_mx8(a.M, a.N, a.x.ld, (int)sizeof(T));
     Mx8Args<T> g = {};
     g.a = a.x.q;
     g.as = a.x.s;
@@ -131,13 +130,19 @@ hipError_t launch_mx8_forward(const Mx8Fwd& a, void* ws, hipStream_t st) {
     g.M = a.M;
     g.N = a.N;
     g.ld = a.x.ld;
-    g.kper = c.kper;
-    g.splits = c.splits;
-    g.part = c.splits > 1 ? static_cast<float*>(ws) : nullptr;
     g.e = {static_cast<const T*>(a.b), static_cast<const T*>(a.residual), static_cast<T*>(a.out), nullptr, a.act,
            a.drop};
     g.out8 = a.out8;
     g.pre8 = a.pre8;
+    if (mx8_few_rows(a.M, a.x.ld)) {
+      hipLaunchKernelGGL((mx8_rows<T>), dim3((unsigned)ceil_div(a.N, 32), (unsigned)ceil_div(a.M, 16)), dim3(1024), 0,
+                         st, g);
+      return hipGetLastError();
+    }
+    const Cut c = cut_mx8(a.M, a.N, a.x.ld, (int)sizeof(T));
+    g.kper = c.kper;
+    g.splits = c.splits;
+    g.part = c.splits > 1 ? static_cast<float*>(ws) : nullptr;
     const dim3 grid((unsigned)(8 * ceil_div(c.splits * ceil_div(g.M, c.tile) * ceil_div(g.N, c.tile), 8)));
     if (c.tile == 256) {
       if constexpr (sizeof(T) == 2) hipLaunchKernelGGL(mx8_gemm_tile256, grid, dim3(512), 0, st, g);

@@ -625,6 +625,77 @@ __global__ void __launch_bounds__(512) mx8_gemm_tile256(Mx8Args<bf16> g) {
   mx8_store<bf16, TM, TN>(g, d, acc, m0 + 128 * wm, n0 + 64 * wn, t.split, lane);
 }
 
+// ---------------------------------------------------------------- few rows
+//
+// Up to 16 rows (serving: single tokens), where the weights' bytes are all the time there is: the same matrix instructions on
+// operands straight from memory, each weight read once.  A workgroup takes 32 columns and 16 rows (blockIdx.y); its 16
+// waves take stages of 128 k's in turn, the loads of two under way, and their sums meet in the LDS, added in order.
+template <typename T>
+__global__ void __launch_bounds__(1024) mx8_rows(Mx8Args<T> g) {
+  constexpr bool WIDE = sizeof(T) == 4;
+  constexpr int NW = 16, PF = 2;
+  __shared__ float sums[NW][512];
+  const int lane = threadIdx.x & 63, gq = lane >> 4, l16 = lane & 15;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const int64_t n0 = (int64_t)blockIdx.x * 32, m0 = (int64_t)blockIdx.y * 16, sld = g.ld / kBlock8;
+  // rows behind the last read that one, for products that are not stored; columns dealt as Slab8's
+  const int64_t xr = min(m0 + l16, g.M - 1);
+  const uint8_t *x = g.a + xr * g.ld, *xs = g.as + xr * sld, *w[2], *ws[2];
+#pragma unroll
+  for (int b = 0; b < 2; ++b) {
+    const int64_t r = min(n0 + 8 * (l16 >> 2) + 4 * b + (l16 & 3), g.N - 1);
+    w[b] = g.b + r * g.ld;
+    ws[b] = g.bs + r * sld;
+  }
+  auto operand = [&](const uint8_t* p, int64_t k) {
+    Mx8Op o;
+#pragma unroll
+    for (int h = 0; h < 2; ++h) {
+      const int64_t at = k + 16 * (WIDE ? 2 * gq + h : 4 * h + gq);
+      o.u[h] = make_uint4(0, 0, 0, 0);
+      if (at < g.ld) o.u[h] = *reinterpret_cast<const uint4*>(p + at);
+    }
+    return o;
+  };
+  auto scale = [&](const uint8_t* p, int64_t k) { return k / kBlock8 + gq < sld ? (int)p[k / kBlock8 + gq] : 127; };
+  f32x4 acc[1][2] = {{f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}}};
+  for (int64_t k0 = 128 * wave; k0 < g.ld; k0 += 128 * NW * PF) {
+    Mx8Op fx[PF][1], fw[PF][2];
+    int cx[PF][1], cw[PF][2];
+#pragma unroll
+    for (int i = 0; i < PF; ++i) {
+      const int64_t k = k0 + 128 * NW * i;
+      fx[i][0] = operand(x, k);
+      cx[i][0] = scale(xs, k);
+#pragma unroll
+      for (int b = 0; b < 2; ++b) {
+        fw[i][b] = operand(w[b], k);
+        cw[i][b] = scale(ws[b], k);
+      }
+    }
+#pragma unroll
+    for (int i = 0; i < PF; ++i) mx8_products<T>(fx[i], fw[i], cx[i], cw[i], acc, 0);
+  }
+  const int64_t n = n0 + 8 * gq;
+  float o[8], bias[8];
+  load_bias8(g.e, g.N, n, bias);  // the loads of what is wanted last under cover of the sums
+  const Drop d(g.e.drop);
+#pragma unroll
+  for (int i = 0; i < 8; ++i) sums[wave][64 * i + lane] = acc[0][i / 4][i % 4];
+  __syncthreads();
+  if (threadIdx.x < 512) {
+    float s = 0.f;
+#pragma unroll
+    for (int j = 0; j < NW; ++j) s += sums[j][threadIdx.x];
+    sums[0][threadIdx.x] = s;  // nobody else's column
+  }
+  __syncthreads();
+  if (wave) return;
+#pragma unroll
+  for (int i = 0; i < 8; ++i) o[i] = sums[0][64 * i + lane] + bias[i];
+  finish8<T, 8, kRowsApart>(g, d, m0 + l16, n, o, whole_units8(g));
+}
+
 // The splits' sums added in order, then the epilogue; eight neighbouring elements a thread, four threads a block.
 template <typename T>
 __global__ void __launch_bounds__(256) mx8_join_splits(Mx8Args<T> g) {

@@ -87,6 +87,29 @@ def mx8_empty(shape, device) -> Mx8:
                torch.empty((*lead, blocks), dtype=torch.float8_e8m0fnu, device=device), C)
 
 
+def _new8(like, lead, C) -> Mx8:
+    """mx8_empty on the device of a tensor."""
+    import torch
+    blocks = -(-C // BLOCK)
+    return Mx8(like.new_empty((*lead, BLOCK * blocks), dtype=torch.float8_e4m3fn),
+               like.new_empty((*lead, blocks), dtype=torch.float8_e8m0fnu), C)
+
+
+def _fit8(t, lead, C, device) -> bool:
+    """Whether _expect8 would pass an Mx8 (or None): the quick check, as train.py's _fit."""
+    import torch
+    if t is None:
+        return True
+    if type(t) is not Mx8 or t.channels != C:
+        return False
+    values, scales, _ = t
+    blocks = -(-C // BLOCK)
+    return (values.shape == (*lead, BLOCK * blocks) and scales.shape == (*lead, blocks)
+            and values.dtype is torch.float8_e4m3fn and scales.dtype is torch.float8_e8m0fnu
+            and values.device == device and scales.device == device and values.is_cuda
+            and values.is_contiguous() and scales.is_contiguous())
+
+
 def _expect8(name, t, shape, device):
     """Checks, before any GPU call, that t holds a tensor of this shape in eight bits on the device."""
     import torch
@@ -145,11 +168,11 @@ def mx8_pack(x, *, out=None, stream=None) -> Mx8:
     shape = x.shape
     if not _fit(x):
         _expect(x, [])
-    if out is not None:
+    if not _fit8(out, shape[:-1], C, x.device):
         _expect8("out", out, shape, x.device)
 
     def call(handle):
-        y = mx8_empty(shape, x.device) if out is None else out
+        y = _new8(x, shape[:-1], C) if out is None else out
         _check(afno_mx8_pack(_address(x), M, C, code, *_addresses8(y), handle))
         return y
 
@@ -162,7 +185,8 @@ def mx8_unpack(x: Mx8, *, dtype=None, out=None, stream=None):
     import torch
     shape = _shape8("x", x)
     values = x.values
-    _expect8("x", x, shape, values.device)
+    if not _fit8(x, shape[:-1], shape[-1], values.device):
+        _expect8("x", x, shape, values.device)
     if dtype is None:
         dtype = torch.bfloat16 if out is None else out.dtype
     if out is not None:
@@ -189,7 +213,7 @@ def rms_norm_forward(x, gamma, *, eps=1e-6, residual=None, out=None, sum_out=Non
         _expect(x, [("gamma", gamma, (C,), None)] + [
             (n, t, tuple(shape), None) for n, t in (("residual", residual), ("out", out), ("sum_out", sum_out))
             if t is not None])
-    if out8 is not None:
+    if not _fit8(out8, shape[:-1], C, x.device):
         _expect8("out8", out8, shape, x.device)
 
     def call(handle):
@@ -233,18 +257,20 @@ def mx8_linear_forward(x: Mx8, w: Mx8, b=None, *, activation="none", residual=No
     if w is None or len(_shape8("w", w)) != 2:
         raise ValueError("w must be an Mx8 of [N, K]")
     values, N = x.values, w.values.shape[0]
-    shape = (*lead, N)
-    _expect8("x", x, (*lead, K), values.device)
-    _expect8("w", w, (N, K), values.device)
+    shape, device = (*lead, N), values.device
+    if not (_fit8(x, lead, K, device) and _fit8(w, (N,), K, device) and _fit8(out8, lead, N, device)
+            and _fit8(pre8, lead, N, device)):
+        _expect8("x", x, (*lead, K), device)
+        _expect8("w", w, (N, K), device)
+        for n, t in (("out8", out8), ("pre8", pre8)):
+            if t is not None:
+                _expect8(n, t, shape, device)
     if dtype is None:
         dtype = next((t.dtype for t in (out, b, residual) if t is not None), torch.bfloat16)
-    given = [(n, t, s, dtype) for n, t, s in (("b", b, (N,)), ("residual", residual, shape), ("out", out, shape))
-             if t is not None]
-    _expect(values, given)
     code = _code(dtype)
-    for n, t in (("out8", out8), ("pre8", pre8)):
-        if t is not None:
-            _expect8(n, t, shape, values.device)
+    for n, t, s in (("b", b, (N,)), ("residual", residual, shape), ("out", out, shape)):
+        if t is not None and (t.shape != s or t.dtype != dtype or t.device != device or not t.is_contiguous()):
+            _expect(values, [(n, t, s, dtype)])
     act, drop = _activation(activation), _random(values, p, seed, offset, counter)
     M = x.scales.numel() // x.scales.shape[-1]
 
@@ -278,8 +304,9 @@ def mx8_linear_backward(g, x: Mx8, w, *, pre8=None, activation="none", p=0.0, se
         raise ValueError("w has no columns")
     if g.shape != shape or not _fit(g, (w, (K, N))):
         _expect(g, [("g", g, shape, None), ("w", w, (K, N), None)])
-    _expect8("x", x, (*lead, K), g.device)
-    if act:
+    if not _fit8(x, lead, K, g.device):
+        _expect8("x", x, (*lead, K), g.device)
+    if act and (pre8 is None or not _fit8(pre8, lead, N, g.device)):
         _expect8("pre8", pre8, shape, g.device)
     if not (bias or need_dx or need_dw):
         raise ValueError("no gradient is asked for")
