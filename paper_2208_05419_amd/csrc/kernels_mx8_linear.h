@@ -504,20 +504,19 @@ __global__ void __launch_bounds__(512) mx8_gemm_tile256(Mx8Args<bf16> g) {
   __shared__ uint4 st0[SA::U + SB::U];
   __shared__ uint4 st1[SA::U + SB::U];
   __shared__ uint4 scales[2][512];
-  const TilePlace t((g.M + 255) / 256, (g.N + 255) / 256, g.splits);
+  const TilePlace t((g.M + 255) / 256, (g.N + 255) / 256, 1);
   if (!t.any) return;
   const int64_t m0 = t.m * 256, n0 = t.n * 256;
-  const int64_t k0 = t.split * g.kper, k1 = min(g.ld, k0 + g.kper);
   const int tid = threadIdx.x, lane = tid & 63, gq = lane >> 4, l16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6), wm = wave >> 2, wn = wave & 3;
-  const int S = (int)((k1 - k0) / BK), left = (int)(k1 - k0 - (int64_t)S * BK);  // whole stages, the rest
+  const int S = (int)(g.ld / BK), left = (int)(g.ld - (int64_t)S * BK);  // whole stages, the rest
   const SA sa(g.a, g.as, g.ld, m0, g.M, tid, wm);
   const SB sb(g.b, g.bs, g.ld, n0, g.N, tid, wn);
-  // the row whose scales this thread loads: of a, then of b.  The last four stages' 16 bytes are the last 16 of the
-  // split's, with those of fewer stages behind `shift` earlier ones.
-  const int blocks = (int)((k1 - k0) / kBlock8);
-  const uint8_t* from = (wave < 4 ? g.as + m0 * (g.ld / kBlock8) : g.bs + n0 * (g.ld / kBlock8)) + k0 / kBlock8;
-  const uint32_t row = (uint32_t)min((int64_t)(tid & 255), (wave < 4 ? g.M - m0 : g.N - n0) - 1) * (uint32_t)(g.ld / kBlock8);
+  // the row whose scales this thread loads: of a, then of b.  The last four stages' 16 bytes are the row's last 16, with
+  // those of fewer stages behind `shift` earlier ones.
+  const int blocks = (int)(g.ld / kBlock8);
+  const uint8_t* from = wave < 4 ? g.as + m0 * blocks : g.bs + n0 * blocks;
+  const uint32_t row = (uint32_t)min((int64_t)(tid & 255), (wave < 4 ? g.M - m0 : g.N - n0) - 1) * (uint32_t)blocks;
   // this wave's places in them
   const int pa = 16 * (128 * wm + l16) + gq, pb = 16 * (256 + 64 * wn + SB::NV * (l16 >> 2) + (l16 & 3)) + gq;
 
@@ -542,7 +541,7 @@ __global__ void __launch_bounds__(512) mx8_gemm_tile256(Mx8Args<bf16> g) {
   auto stage = [&](const uint4* st, uint4* next, int first, int j, auto more, auto rest) {
     const int shift = first ? 4 * first - min(4 * first, blocks - 16) : 0;
     const int sc = 16 * 512 * (first >> 2 & 1) + shift + 4 * j;
-    const int64_t kn = k0 + (int64_t)min(first + j + 1, S - 1) * BK;  // behind the last: that again, nobody reads it
+    const int64_t kn = (int64_t)min(first + j + 1, S - 1) * BK;  // behind the last: that again, nobody reads it
     const auto rb = sb.read(st + SA::U);
     const auto ra = sa.read(st);
     // all scales ahead of the loads into the LDS: the compiler waits for those before it reads an array that it does not
@@ -575,8 +574,8 @@ __global__ void __launch_bounds__(512) mx8_gemm_tile256(Mx8Args<bf16> g) {
     }
   };
   if (S) {
-    sa.issue(st0 + 64 * wave, k0);
-    sb.issue(st0 + SA::U + 64 * wave, k0);
+    sa.issue(st0 + 64 * wave, 0);
+    sb.issue(st0 + SA::U + 64 * wave, 0);
   }
   if (blocks >= 16) {
     __builtin_memcpy(&next_scales, from + row, 16);
@@ -609,7 +608,7 @@ __global__ void __launch_bounds__(512) mx8_gemm_tile256(Mx8Args<bf16> g) {
     if (wave < 4) dma_barrier();
   }
   if (left > 0) {
-    const int64_t k = k0 + (int64_t)S * BK;
+    const int64_t k = (int64_t)S * BK;
     sync();
     sa.issue_rest(st0 + 64 * wave, k, left, tid);
     sb.issue_rest(st0 + SA::U + 64 * wave, k, left, tid);
@@ -622,7 +621,7 @@ __global__ void __launch_bounds__(512) mx8_gemm_tile256(Mx8Args<bf16> g) {
   asm volatile("" ::: "memory");
   __builtin_amdgcn_s_waitcnt(wait_loads(0));
   asm volatile("" ::: "memory");
-  mx8_store<bf16, TM, TN>(g, d, acc, m0 + 128 * wm, n0 + 64 * wn, t.split, lane);
+  mx8_store<bf16, TM, TN>(g, d, acc, m0 + 128 * wm, n0 + 64 * wn, 0, lane);
 }
 
 // ---------------------------------------------------------------- few rows
