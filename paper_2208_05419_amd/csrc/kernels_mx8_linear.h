@@ -183,13 +183,27 @@ __device__ __forceinline__ uint32_t turn_scales(uint32_t w, uint32_t sel) {
                                0x05040100u);
 }
 
-// NV (8 or 16) neighbouring values of row m from column n on, in eight bits; JOIN, which lanes have the rest of the
+// A place in a product's results: row and column, and what lies ahead of it in rows of N values, of ld bytes and of scales (products
+// of 64 bits, 32 cycles a wave each: taken once, and from row tile to row tile by addition).
+struct Place8 {
+  int64_t m, n, at, q, s;
+  __device__ __forceinline__ Place8(int64_t m, int64_t n, int64_t N)
+      : m(m), n(n), at(m * N + n), q(m * row8(N) + n), s(m * (row8(N) / kBlock8) + n / kBlock8) {}
+  __device__ __forceinline__ void down(int rows, int64_t N) {
+    m += rows;
+    at += rows * N;
+    q += rows * row8(N);
+    s += rows * (row8(N) / kBlock8);
+  }
+};
+
+// NV (8 or 16) neighbouring values from a place on, in eight bits; JOIN, which lanes have the rest of the
 // block: the next ones, the ones 16 apart, the one 32 apart.  All lanes of the wave together.  there: the row exists
 // (columns behind the last are not stored).
 enum { kNeighbours, kRowsApart, kHalves };
 template <int NV, int JOIN>
-__device__ __forceinline__ void store8(const Rows8& o, int64_t m, int64_t n, int64_t N, const float (&z)[NV],
-                                       bool there) {
+__device__ __forceinline__ void store8(const Rows8& o, const Place8& p, int64_t N, const float (&z)[NV], bool there) {
+  const int64_t n = p.n;
   float v[NV];
 #pragma unroll
   for (int i = 0; i < NV; ++i) v[i] = z[i];
@@ -204,10 +218,10 @@ __device__ __forceinline__ void store8(const Rows8& o, int64_t m, int64_t n, int
   uint32_t w[NV / 4];
   round8(v, byte, w);
   if (!there || n >= o.ld) return;
-  uint8_t* q = o.q + m * o.ld + n;
+  uint8_t* q = o.q + p.q;
   if constexpr (NV == 8) *reinterpret_cast<uint2*>(q) = make_uint2(w[0], w[1]);
   else *reinterpret_cast<uint4*>(q) = make_uint4(w[0], w[1], w[2], w[3]);
-  if (n % kBlock8 == 0) o.s[m * (o.ld / kBlock8) + n / kBlock8] = (uint8_t)byte;
+  if (n % kBlock8 == 0) o.s[p.s] = (uint8_t)byte;
 }
 
 // NV values of type T in registers
@@ -226,11 +240,12 @@ union Some {
 // The epilogue of NV neighbouring values, their biases added; as store8 all lanes of the wave together.  In bf16 the
 // short GELU, whose error is below that of the eight-bit instruction (64,800 x 1,024 x 4,096: @@ us, @@ with the other one).
 template <typename T, int NV, int JOIN>
-__device__ __forceinline__ void finish8(const Mx8Args<T>& g, const Drop& d, int64_t m, int64_t n,
-                                        float (&o)[NV], bool units) {
+__device__ __forceinline__ void finish8(const Mx8Args<T>& g, const Drop& d, const Place8& p, float (&o)[NV],
+                                        bool units) {
   const Epilogue<T>& e = g.e;
-  const bool there = m < g.M;
-  if (g.pre8.q) store8<NV, JOIN>(g.pre8, m, n, g.N, o, there);
+  const bool there = p.m < g.M;
+  const int64_t n = p.n, at = p.at;
+  if (g.pre8.q) store8<NV, JOIN>(g.pre8, p, g.N, o, there);
   if (e.act == kActGelu) {
 #pragma unroll
     for (int i = 0; i < NV; ++i) o[i] = sizeof(T) == 2 ? gelu_short(o[i]) : gelu(o[i]);
@@ -238,7 +253,6 @@ __device__ __forceinline__ void finish8(const Mx8Args<T>& g, const Drop& d, int6
 #pragma unroll
     for (int i = 0; i < NV; ++i) o[i] = activate(o[i], kActRelu);
   }
-  const int64_t at = m * g.N + n;
   if (d.threshold) {
 #pragma unroll
     for (int h = 0; h < NV / 8; ++h) {
@@ -268,8 +282,7 @@ __device__ __forceinline__ void finish8(const Mx8Args<T>& g, const Drop& d, int6
 #pragma unroll
       for (int i = 0; i < S::NU; ++i) {
         if (units)
-          __builtin_nontemporal_store((Words){r.u[i].x, r.u[i].y, r.u[i].z, r.u[i].w},
-                                      reinterpret_cast<Words*>(e.out + at + S::UE * i));
+          *reinterpret_cast<Words*>(e.out + at + S::UE * i) = (Words){r.u[i].x, r.u[i].y, r.u[i].z, r.u[i].w};
         else
           __builtin_memcpy(e.out + at + S::UE * i, &r.u[i], 16);
       }
@@ -279,7 +292,7 @@ __device__ __forceinline__ void finish8(const Mx8Args<T>& g, const Drop& d, int6
         if (n + i < g.N) e.out[at + i] = r.e[i];
     }
   }
-  if (g.out8.q) store8<NV, JOIN>(g.out8, m, n, g.N, o, there);
+  if (g.out8.q) store8<NV, JOIN>(g.out8, p, g.N, o, there);
 }
 template <typename T, int NV>
 __device__ __forceinline__ void load_bias8(const Epilogue<T>& e, int64_t N, int64_t n, float (&b)[NV]) {
@@ -296,14 +309,15 @@ __device__ __forceinline__ bool whole_units8(const Mx8Args<T>& g) {
 
 // NV neighbouring sums of row m from column n on: a split's, or the results.  All lanes of the wave together.
 template <typename T, int NV, int JOIN>
-__device__ __forceinline__ void mx8_out(const Mx8Args<T>& g, const Drop& d, int64_t m, int64_t n, int split,
+__device__ __forceinline__ void mx8_out(const Mx8Args<T>& g, const Drop& d, const Place8& at, int split,
                                         float (&o)[NV], bool units) {
   if (!g.part) {
-    finish8<T, NV, JOIN>(g, d, m, n, o, units);
+    finish8<T, NV, JOIN>(g, d, at, o, units);
     return;
   }
-  if (m >= g.M) return;
-  float* p = g.part + (split * g.M + m) * g.N + n;
+  if (at.m >= g.M) return;
+  const int64_t n = at.n;
+  float* p = g.part + split * g.M * g.N + at.at;
   if (g.N % 4 == 0) {
 #pragma unroll
     for (int i = 0; i < NV / 4; ++i)
@@ -340,15 +354,15 @@ __device__ __forceinline__ void mx8_store(const Mx8Args<T>& g, const Drop& d, co
   if (n0 >= g.N) return;  // the whole wave's
   const int l16 = lane & 15, gq = lane >> 4;
   const bool units = whole_units8(g);
-  const int64_t n = n0 + NV * gq;
+  Place8 p(m0 + l16, n0 + NV * gq, g.N);
 #pragma unroll
   for (int a = 0; a < TM; ++a) {
-    const int64_t m = m0 + 16 * a + l16;
     __builtin_amdgcn_sched_barrier(0);  // one group's values at a time in registers
     float o[NV];
 #pragma unroll
     for (int i = 0; i < NV; ++i) o[i] = acc[a][i / 4][i % 4];
-    mx8_out<T, NV, kRowsApart>(g, d, m, n, split, o, units);
+    mx8_out<T, NV, kRowsApart>(g, d, p, split, o, units);
+    p.down(16, g.N);
   }
 }
 
@@ -692,7 +706,7 @@ __global__ void __launch_bounds__(1024) mx8_rows(Mx8Args<T> g) {
   if (wave) return;
 #pragma unroll
   for (int i = 0; i < 8; ++i) o[i] = sums[0][64 * i + lane] + bias[i];
-  finish8<T, 8, kRowsApart>(g, d, m0 + l16, n, o, whole_units8(g));
+  finish8<T, 8, kRowsApart>(g, d, Place8(m0 + l16, n, g.N), o, whole_units8(g));
 }
 
 // The splits' sums added in order, then the epilogue; eight neighbouring elements a thread, four threads a block.
@@ -726,7 +740,7 @@ __global__ void __launch_bounds__(256) mx8_join_splits(Mx8Args<T> g) {
   load_bias8(g.e, g.N, n, bias);
 #pragma unroll
   for (int i = 0; i < 8; ++i) v[i] += bias[i];
-  finish8<T, 8, kNeighbours>(g, d, m, n, v, whole_units8(g));
+  finish8<T, 8, kNeighbours>(g, d, Place8(m, n, g.N), v, whole_units8(g));
 }
 
 }  // namespace afno
