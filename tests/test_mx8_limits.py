@@ -222,3 +222,19 @@ def test_packed_rows_of_a_larger_tensor():
     assert torch.equal(afno.mx8_linear_forward(part, w8), afno.mx8_linear_forward(x8, w8)[13:50])
     grid = afno.Mx8(x8.values.reshape(7, 10, 352), x8.scales.reshape(7, 10, 11), 333)
     assert torch.equal(afno.mx8_linear_forward(grid, w8), afno.mx8_linear_forward(x8, w8).reshape(7, 10, 40))
+
+
+def test_norm_of_a_sum_past_float32_and_of_zeros_without_eps():
+    """A row whose sum of squares float32 does not hold gives zeros and passes gsum on; 0 / 0 is NaN; other rows as alone."""
+    x = torch.randn(4, 64, device="cuda")
+    x[1], x[2] = 1e19, 0.0  # 64e38 and 0
+    ga, g = torch.ones(64, device="cuda"), torch.randn(4, 64, device="cuda")
+    out, out8 = torch.empty_like(x), afno.mx8_empty((4, 64), "cuda")
+    afno.rms_norm_forward(x, ga, eps=0.0, out=out, out8=out8)
+    dx = afno.rms_norm_backward(g, x, ga, eps=0.0, gsum=g)["dx"]
+    got8 = afno.mx8_unpack(out8, dtype=torch.float32)
+    assert not out[1].any() and not got8[1].any() and torch.equal(dx[1], g[1])
+    assert torch.isnan(out[2]).all() and torch.isnan(got8[2]).all() and torch.isnan(dx[2]).all()
+    for i in (0, 3):
+        assert torch.equal(out[i], afno.rms_norm_forward(x[i:i + 1], ga, eps=0.0)[0])
+        assert torch.equal(dx[i], afno.rms_norm_backward(g[i:i + 1], x[i:i + 1], ga, eps=0.0, gsum=g[i:i + 1])["dx"][0])
