@@ -147,8 +147,8 @@ hipError_t launch_mx8_forward(const Mx8Fwd& a, void* ws, hipStream_t st) {
     const dim3 grid((unsigned)(8 * ceil_div(c.splits * ceil_div(g.M, c.tile) * ceil_div(g.N, c.tile), 8)));
     if constexpr (sizeof(T) == 2) {
       if (c.tile == 256) hipLaunchKernelGGL(mx8_gemm_tile256, grid, dim3(512), 0, st, g);
-      if (c.tile == 128) hipLaunchKernelGGL((mx8_gemm_tile<T, 128>), grid, dim3(256), 0, st, g);
     }
+    if (c.tile == 128) hipLaunchKernelGGL((mx8_gemm_tile<T, 128>), grid, dim3(256), 0, st, g);
     if (c.tile == 64) hipLaunchKernelGGL((mx8_gemm_tile<T, 64>), grid, dim3(256), 0, st, g);
     if (c.splits > 1)
       hipLaunchKernelGGL((mx8_join_splits<T>), dim3((unsigned)ceil_div(g.M * (row8(g.N) / 8), 256)), dim3(256), 0, st,

@@ -374,9 +374,9 @@ __device__ __forceinline__ void mx8_store(const Mx8Args<T>& g, const Drop& d, co
 // beside the other's products.  A lane group loads the scales of one stage of four as a word a row, which are turned round
 // in registers: with a byte for each stage and row, whose waits come between the stages' loads, 64,800 x 4,096 x 1,024
 // took 769 us for 473 in tiles of 128.  Tiles of 128: 10,368 x 1,536 x 384 with GELU 17 us, 720 TFLOP/s, one tile of twelve
-// stages on nearly every CU: latency and the one epilogue.  Tiles of 64 in fp32: 64,800 x 1,024 x 1,024 with GELU 280 to 320
-// us, 420 to 490 TFLOP/s, two fifths of the bf16 library product's rate, bound by the widening of each operand to bfloat16
-// in every wave that reads it.  Few rows: 64 x 4,096 x 1,024 in four splits 6.4 us, latency.
+// stages on nearly every CU: latency and the one epilogue.  In fp32: 64,800 x 1,024 x 1,024 220 us, 616 TFLOP/s, 16,200 x
+// 4,096 x 1,024 157 us, 867 (matrix cores 32 %), bound by the widening of each operand to bfloat16 in every wave that reads it, the half
+// as often as in tiles of 64 (320 and 211 us).  Few rows: 64 x 4,096 x 1,024 in four splits 6.4 us, latency.
 template <typename T, int TILE>
 __global__ void __launch_bounds__(256, 2) mx8_gemm_tile(Mx8Args<T> g) {
   constexpr int NT = 256, WR = TILE / 2, TM = WR / 16, TN = WR / 16, NS = TILE == 128 ? 2 : 4;

@@ -5,12 +5,13 @@
 
 namespace afno {
 
-// ld: bytes of a row, K rounded up to 32.  Times with GELU, the join of the splits among them.
-// bf16: 256 where some five CUs in eight get a tile of it (9,600 x 1,024 x 1,280, 190 tiles: 28.5 us, 128 35.0; 4,096 x
-// 1,024 x 4,096, 256 tiles: 35.6, 128 42.8; but 4,096 x 1,024 x 2,048, 128 tiles: 26.4 and 23.0, 6,400 x 4,096 x 1,024, 100
-// tiles: 58.1 and 44.9), 128 where three in four get one (10,368 x 1,536 x 384, 243 tiles: 17.9, 64 20.4; 2,100 x 4,096 x
-// 1,024, 136 tiles: 32.7 and 31.5).  fp32: 64, whose four workgroups a CU cover each other's conversions (64,800 x
-// 1,024 x 1,024: 279 us, 128 362; 10,368 x 384 x 1,536 46 and 95; of longer rows, 16,200 x 4,096 x 1,024, 198 and 177).
+// ld: bytes of a row, K rounded up to 32.  Times with GELU, M x 1,024 x 1,024 unless said, the join of the splits among them.
+// bf16, 256: a CU has one workgroup of it and two of 128, so it pays from where those take a second round, more than 512
+// tiles of 128 (576 of them, 9,216 rows: 27.7 us, 128 29.6; of 256 k's 18.2 and 19.3, of 4,096 61.4 and 73.9; but 512: 27.2 and
+// 21.7), but for a second round of its own that is a third full (275 tiles, 17,600 rows: 50.8 and 46.4, of 128 k's 31.6 and
+// 22.7; 350 tiles: 52.2 and 52.6; 512: 55.6 and 69.1).
+// 128 where three in four CUs get a tile (200 tiles: 14.2, 64 17.4; 128 tiles: 13.8 and 10.4), in fp32 but for a few more
+// than the CUs (fp32: 200 tiles 19.9 and 21.5, 256 21.1 and 22.8, 320 29.5 and 27.5, 400 30.7 and 35.0, 4,096 222 and 297).
 // Splits of k where tiles of 64 leave CUs without one, of 1,024 k's at least (64 x 4,096 x 1,024, 16 tiles: 9.7 us in
 // four, 11.6 whole, fp32 13.8 in two and 18.5; 128 x 4,096 x 4,096, 128 tiles: 13.7 in two, 14.3 whole; 64 x
 // 1,024 x 4,096 8.7 in two of 512, 6.3 whole).
@@ -23,8 +24,9 @@ inline Cut cut_mx8(int64_t M, int64_t N, int64_t ld, int es) {
     c.splits = (int)ceil_div(ld, c.kper);
     return c;
   };
-  if (es == 2 && tiles(256) >= 160) return cut(256, 1);
-  if (es == 2 && tiles(128) >= 192) return cut(128, 1);
+  const int64_t t256 = tiles(256), t128 = tiles(128);
+  if (es == 2 && t128 > 512 && (t256 <= 256 || t256 >= 340)) return cut(256, 1);
+  if (t128 >= 192 && (es == 2 || t128 <= 256 || t128 >= 360)) return cut(128, 1);
   const int64_t t = tiles(64);
   return cut(64, t >= 256 ? 1 : std::max<int64_t>(1, std::min<int64_t>(256 / t, ld / 1024)));
 }

@@ -47,6 +47,10 @@ PATHS = [
     ("fp32", 5000, 1100, 300, "gelu", 0.1, True, True),
     ("bf16", 5000, 500, 600, "gelu", 0.1, True, True),      # 128
     ("bf16", 5000, 1100, 600, "relu", 0.0, True, False),
+    ("fp32", 5000, 500, 600, "gelu", 0.1, True, True),
+    ("fp32", 5000, 1100, 600, "relu", 0.0, True, False),
+    ("fp32", 10300, 70, 1030, "gelu", 0.1, False, False),
+    ("fp32", 6000, 384, 600, "none", 0.0, False, True),
     # 256: stages of 128 k's by fours, what is left of them, and of a stage; up to 16 blocks of scales and more
     ("bf16", 10300, 512, 1030, "gelu", 0.1, False, False),
     ("bf16", 10300, 520, 1030, "none", 0.1, True, False),
@@ -86,7 +90,7 @@ def test_every_reachable_kernel_has_a_case(kinds):
     reached = kinds([(es, M, K, N) for es, M, K, N in itertools.product((2, 4), ROWS, WIDTHS, WIDTHS)])
     cases = kinds([(size[c[0]], *c[1:4]) for c in PATHS])
     assert reached == cases
-    assert {(2, "256", False), (2, "128", False), (4, "64", True)} <= reached and os.path.isdir(CSRC)
+    assert {(2, "256", False), (2, "128", False), (4, "64", True), (4, "128", False)} <= reached and os.path.isdir(CSRC)
 
 
 @pytest.mark.gpu
