@@ -5,8 +5,8 @@
 // bf16: the matrix cores' scaled instruction, which multiplies 16 x 16 tiles over 128 k's of E4M3 values and
 // applies the scales of x and w itself, at twice the rate of bf16.  v_mfma_scale_f32_16x16x128_f8f6f4: lane
 // l = 16 gq + l16 gives of row l16 the k's 16 gq .. + 15 and 64 + 16 gq .. + 15 (measured: with a byte of one lane set
-// and the scales of all lanes distinct), and the scale of that row's block gq, k's 32 gq .. + 31.  Its sums are in float32 but
-// for one place: of eight neighbouring k's products the instruction drops what lies below 2^-13 of the
+// and the scales of all lanes distinct), and the scale of that row's block gq, k's 32 gq .. + 31.  Its sums are in float32
+// but for one place: of eight neighbouring k's products the instruction drops what lies below 2^-13 of the
 // power of two in the largest (measured: 1 + 2^-13 is kept, 1 + 2^-14 is not, nor any number of them; the unscaled
 // instruction does so too), 1.7e-5 of the result in the relative 2-norm at any K, where bfloat16 rounds off 1.7e-3 and
 // E4M3 2.6e-2.
@@ -98,7 +98,8 @@ struct Slab8 {
   static constexpr int CH = 8, U = W * CH, L = U / NT;  // chunks of a row, 16-byte units, loads a lane
   static_assert(U % NT == 0, "whole loads");
   Buf base;  // the workgroup's rows
-  uint32_t at, last, far;  // this lane's first load, bytes behind a stage's base, its place in the last row; from load to load
+  // this lane's first load, bytes behind a stage's base, its place in the last row; from load to load
+  uint32_t at, last, far;
   int v[2];                // this lane's operand places, bytes into the slab
   const uint8_t* scales;   // of the workgroup's first row
   uint32_t sat, step, most;  // this lane's row of the first tile in them, from tile to tile, the last row
@@ -375,8 +376,8 @@ __device__ __forceinline__ void mx8_store(const Mx8Args<T>& g, const Drop& d, co
 // in registers: with a byte for each stage and row, whose waits come between the stages' loads, 64,800 x 4,096 x 1,024
 // took 769 us for 473 in tiles of 128.  Tiles of 128: 10,368 x 1,536 x 384 with GELU 17 us, 720 TFLOP/s, one tile of twelve
 // stages on nearly every CU: latency and the one epilogue.  In fp32: 64,800 x 1,024 x 1,024 220 us, 616 TFLOP/s, 16,200 x
-// 4,096 x 1,024 157 us, 867 (matrix cores 32 %), bound by the widening of each operand to bfloat16 in every wave that reads it, the half
-// as often as in tiles of 64 (320 and 211 us).  Few rows: 64 x 4,096 x 1,024 in four splits 6.4 us, latency.
+// 4,096 x 1,024 157 us, 867 (matrix cores 32 %), bound by the widening of each operand to bfloat16 in every wave that reads
+// it, half as often as in tiles of 64 (320 and 211 us).  Few rows: 64 x 4,096 x 1,024 in four splits 6.4 us, latency.
 template <typename T, int TILE>
 __global__ void __launch_bounds__(256, 2) mx8_gemm_tile(Mx8Args<T> g) {
   constexpr int NT = 256, WR = TILE / 2, TM = WR / 16, TN = WR / 16, NS = TILE == 128 ? 2 : 4;
