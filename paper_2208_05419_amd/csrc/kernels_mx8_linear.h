@@ -16,6 +16,7 @@
 #pragma once
 #include "kernels_linear_dma.h"
 #include "mx8.h"
+#include "mx8_rules.h"
 
 namespace afno {
 
@@ -532,7 +533,7 @@ __global__ void __launch_bounds__(512) mx8_gemm_tile256(Mx8Args<bf16> g) {
   typedef Slab8<true, false, 256, 64, 512> SB;
   __shared__ uint4 st0[SA::U + SB::U];
   __shared__ uint4 st1[SA::U + SB::U];
-  __shared__ uint4 scales[2][512];
+  __shared__ uint4 scales[2][kScaleRows256];
   const TilePlace t((g.M + 255) / 256, (g.N + 255) / 256, 1);
   if (!t.any) return;
   const int64_t m0 = t.m * 256, n0 = t.n * 256;
@@ -568,8 +569,7 @@ __global__ void __launch_bounds__(512) mx8_gemm_tile256(Mx8Args<bf16> g) {
   const std::integral_constant<bool, true> yes;
   const std::integral_constant<bool, false> no;
   auto stage = [&](const uint4* st, uint4* next, int first, int j, auto more, auto rest) {
-    const int shift = first ? 4 * first - min(4 * first, blocks - 16) : 0;
-    const int sc = 16 * 512 * (first >> 2 & 1) + shift + 4 * j;
+    const int sc = scales_at256(first, j, blocks) - (decltype(rest)::value ? scale_back256(gq, left / kBlock8) : 0);
     const int64_t kn = (int64_t)min(first + j + 1, S - 1) * BK;  // behind the last: that again, nobody reads it
     const auto rb = sb.read(st + SA::U);
     const auto ra = sa.read(st);
@@ -622,7 +622,7 @@ __global__ void __launch_bounds__(512) mx8_gemm_tile256(Mx8Args<bf16> g) {
     int s = 0;
     // no way out or branch inside the loop: with one, the accumulators live in two sets of registers
     for (; s + 3 < S; s += 4) {
-      __builtin_memcpy(&next_scales, from + row + min(4 * s + 16, blocks - 16), 16);
+      __builtin_memcpy(&next_scales, from + row + next_scales256(s, blocks), 16);
       stage(st0, st1, s, 0, yes, no);
       stage(st1, st0, s, 1, yes, no);
       scales[(s >> 2 & 1) ^ 1][tid] = next_scales;

@@ -37,4 +37,19 @@ inline size_t mx8_part_bytes(int64_t M, int64_t N, int64_t ld, int es) {
   return mx8_few_rows(M, ld) ? 0 : part_of(M, N, cut_mx8(M, N, ld, es));
 }
 
+// The scales that mx8_gemm_tile256 has in the LDS: of each of its 512 rows 16 bytes, in one of two buffers for stages `first`
+// .. first + 3 (first a multiple of four).  Rows of `blocks` scales; 16 of them at least from the fourth stage on.
+constexpr int kScaleRows256 = 512;
+// the row's block in the first of the 16 bytes of the stages behind `first` .. + 3: theirs, or what leaves the load within the
+// row (of stages 0 .. 3: block 0)
+constexpr int next_scales256(int first, int blocks) { return std::min(4 * first + 16, blocks - 16); }
+// where the first block of stage first + j is, from the buffers' begin on; rows are 16 bytes apart
+constexpr int scales_at256(int first, int j, int blocks) {
+  const int shift = first ? 4 * first - std::min(4 * first, blocks - 16) : 0;
+  return 16 * kScaleRows256 * (first >> 2 & 1) + shift + 4 * j;
+}
+// how far ahead of block gq lane group gq reads where `there` of a stage's four are there: the last one for those behind it,
+// whose own place would be in the next row, or behind the array
+constexpr int scale_back256(int gq, int there) { return gq < there ? 0 : gq - (there - 1); }
+
 }  // namespace afno
