@@ -356,7 +356,7 @@ int afno_mx8_unpack(const void* values, const void* scales, int64_t M, int64_t C
  *   out [M][C] or NULL   dtype;  out_values, out_scales: out in eight bits, or NULL; one of the two at least
  *   sum [M][C] or NULL   dtype: v, the residual stream and what the gradient takes
  * The sum of v^2 is float32's: in a row where it passes 2^128 the results are 0 (the gradient's, too, but for
- * gsum).  eps 0: a row of zeros gives NaN.
+ * gsum); rows as small as the type holds keep their digits whatever eps is.  eps 0: a row of zeros gives NaN.
  */
 int afno_rms_norm_forward(const void* x, const void* residual, const void* gamma, int64_t M, int64_t C,
                           float eps, int dtype, void* out, void* sum, void* out_values,

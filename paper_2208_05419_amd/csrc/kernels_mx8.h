@@ -74,15 +74,36 @@ __global__ void __launch_bounds__(256) mx8_unpack_kernel(const uint8_t* __restri
 
 // ---------------------------------------------------------------- the norm
 
-// 1 / sqrt(mean(v^2) + eps) of a row; v is 0 behind its channels
+// Small rows: where the mean square and eps lie below 2^-100, squares of float32 lose digits or vanish (eps 0: a row of
+// 1e-23 would divide by 0).  There everything is taken 2^100 times as large, exactly: the largest square is then below
+// 2^20 2^100 (2^20 channels), that of the smallest number 2^-98.  The factor 2^100 of 1 / sqrt() stays apart, since
+// float32 does not hold it for the smallest rows.  Others keep their steps and their bits; the test costs a scalar branch a row.
+constexpr float kSmallRow = 0x1p-100f, kRowUp = 0x1p100f, kRowHalfUp = 0x1p50f;
+__device__ __forceinline__ bool small_row(float mean_and_eps) {
+  return __builtin_amdgcn_readfirstlane(mean_and_eps < kSmallRow);  // the same in the row's threads
+}
+// 1 / sqrt(mean(v^2) + eps) of a row; v is 0 behind its channels.  Of a small row v comes back times kRowUp, and the result is
+// for that.
 template <int W, int NU, int UE>
-__device__ __forceinline__ float row_rms(const float (&v)[NU][UE], int C, float eps, float* s4) {
-  float q = 0.f;
+__device__ __forceinline__ float row_rms(float (&v)[NU][UE], int C, float eps, float* s4, bool* small) {
+  auto mean = [&]() {
+    float q = 0.f;
 #pragma unroll
-  for (int i = 0; i < NU; ++i)
+    for (int i = 0; i < NU; ++i)
 #pragma unroll
-    for (int e = 0; e < UE; ++e) q = __builtin_fmaf(v[i][e], v[i][e], q);
-  return rsqrtf(row_sum<W>(q, s4) / (float)C + eps);
+      for (int e = 0; e < UE; ++e) q = __builtin_fmaf(v[i][e], v[i][e], q);
+    return row_sum<W>(q, s4) / (float)C;
+  };
+  float s = mean() + eps;
+  *small = small_row(s);
+  if (*small) {
+#pragma unroll
+    for (int i = 0; i < NU; ++i)
+#pragma unroll
+      for (int e = 0; e < UE; ++e) v[i][e] *= kRowUp;
+    s = mean() + eps * kRowUp * kRowUp;
+  }
+  return rsqrtf(s);
 }
 
 // UE neighbouring values of each of the 32 / UE lanes of a block, to eight bits at channel c of a row
@@ -137,7 +158,8 @@ __global__ void __launch_bounds__(256) rms_rows(const T* __restrict__ x, const T
     }
     if (sum) P::store(sum + m * C + c, v[i]);
   }
-  const float rms = row_rms<W>(v, C, eps, s4);
+  bool small;
+  const float rms = row_rms<W>(v, C, eps, s4, &small);
 #pragma unroll
   for (int i = 0; i < NU; ++i) {
     const int c = UE * (lane + P::NL * i);
@@ -203,7 +225,8 @@ __global__ void __launch_bounds__(256) rms_rows_backward(const T* __restrict__ g
       if (gsum) P::widen(rs[i], o[i]);
     }
     if (m + step < M) fetch(m + step);
-    const float rms = row_rms<W>(v, C, eps, s4);
+    bool small;
+    float rms = row_rms<W>(v, C, eps, s4, &small);
     float q = 0.f;
 #pragma unroll
     for (int i = 0; i < NU; ++i)
@@ -215,12 +238,14 @@ __global__ void __launch_bounds__(256) rms_rows_backward(const T* __restrict__ g
         q = __builtin_fmaf(a[i][e], v[i][e], q);
       }
     q = row_sum<W>(q, s4) * inv;
+    const float up = small ? kRowHalfUp : 1.f;
+    rms *= up;
 #pragma unroll
     for (int i = 0; i < NU; ++i) {
       const int c = UE * (lane + P::NL * i);
       if (c >= C) continue;
 #pragma unroll
-      for (int e = 0; e < UE; ++e) o[i][e] += rms * (a[i][e] - v[i][e] * q);
+      for (int e = 0; e < UE; ++e) o[i][e] += rms * (up * (a[i][e] - v[i][e] * q));
       P::store(dx + m * C + c, o[i]);
     }
   }
@@ -268,17 +293,27 @@ __global__ void __launch_bounds__(256) rms_wide(const T* __restrict__ x, const T
     if (sum) sum[base + c] = Store<T>::to(v);
     q = __builtin_fmaf(v, v, q);
   }
-  const float rms = rsqrtf(group_sum(q, s4) / (float)C + eps);
+  float mean = group_sum(q, s4) / (float)C + eps, up = 1.f;
+  if (small_row(mean)) {
+    up = kRowUp;
+    q = 0.f;
+    for (int c = threadIdx.x; c < C; c += 256) {
+      const float v = at(c) * up;
+      q = __builtin_fmaf(v, v, q);
+    }
+    mean = group_sum(q, s4) / (float)C + eps * up * up;
+  }
+  const float rms = rsqrtf(mean);
   const int ld = (int)row8(C);  // whole blocks: the 32 lanes of one are in the loop together
   for (int c = threadIdx.x; c < ld; c += 256) {
-    float y[1] = {c < C ? at(c) * rms * ld_f(gamma + c) : 0.f};
+    float y[1] = {c < C ? at(c) * up * rms * ld_f(gamma + c) : 0.f};
     if (out && c < C) out[base + c] = Store<T>::to(y[0]);
     if (o.q) put8(o, m, c, y, true);
   }
 }
 
-// as rms_wide; rms of each row left in stats for rms_columns (2,000 x 9,001 bf16:
-// 45 us, 2.4 TB/s)
+// as rms_wide; rms of each row left in stats for rms_columns, of a small row that of the enlarged one with a minus
+// sign (2,000 x 9,001 bf16: 45 us, 2.4 TB/s)
 template <typename T>
 __global__ void __launch_bounds__(256) rms_wide_backward(const T* __restrict__ g, const T* __restrict__ x,
                                                          const T* __restrict__ gamma, const T* __restrict__ gsum,
@@ -291,14 +326,25 @@ __global__ void __launch_bounds__(256) rms_wide_backward(const T* __restrict__ g
     const float v = ld_f(x + base + c);
     q = __builtin_fmaf(v, v, q);
   }
-  const float rms = rsqrtf(group_sum(q, s4) / (float)C + eps);
-  if (threadIdx.x == 0) stats[blockIdx.x] = rms;
+  float mean = group_sum(q, s4) / (float)C + eps, up = 1.f, half = 1.f;
+  if (small_row(mean)) {
+    up = kRowUp;
+    half = kRowHalfUp;
+    q = 0.f;
+    for (int c = threadIdx.x; c < C; c += 256) {
+      const float v = ld_f(x + base + c) * up;
+      q = __builtin_fmaf(v, v, q);
+    }
+    mean = group_sum(q, s4) / (float)C + eps * up * up;
+  }
+  const float rms = rsqrtf(mean);
+  if (threadIdx.x == 0) stats[blockIdx.x] = up == 1.f ? rms : -rms;
   float s = 0.f;
   for (int c = threadIdx.x; c < C; c += 256)
-    s = __builtin_fmaf(ld_f(g + base + c) * ld_f(gamma + c), ld_f(x + base + c) * rms, s);
+    s = __builtin_fmaf(ld_f(g + base + c) * ld_f(gamma + c), ld_f(x + base + c) * up * rms, s);
   s = group_sum(s, s4) / (float)C;
   for (int c = threadIdx.x; c < C; c += 256) {
-    float d = rms * (ld_f(g + base + c) * ld_f(gamma + c) - ld_f(x + base + c) * rms * s);
+    float d = half * rms * (half * (ld_f(g + base + c) * ld_f(gamma + c) - ld_f(x + base + c) * up * rms * s));
     if (gsum) d += ld_f(gsum + base + c);
     dx[base + c] = Store<T>::to(d);
   }
@@ -313,7 +359,10 @@ __global__ void __launch_bounds__(256) rms_columns(const T* __restrict__ g, cons
   if (c >= C) return;
   const int64_t m0 = blockIdx.y * rows, m1 = min(M, m0 + rows);
   float s = 0.f;
-  for (int64_t m = m0; m < m1; ++m) s = __builtin_fmaf(ld_f(g + m * C + c), ld_f(x + m * C + c) * stats[m], s);
+  for (int64_t m = m0; m < m1; ++m) {
+    const float rms = stats[m], up = rms < 0.f ? kRowUp : 1.f;
+    s = __builtin_fmaf(ld_f(g + m * C + c), ld_f(x + m * C + c) * up * fabsf(rms), s);
+  }
   part[(int64_t)blockIdx.y * C + c] = s;
 }
 
