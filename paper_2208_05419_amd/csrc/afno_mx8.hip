@@ -137,7 +137,7 @@ hipError_t launch_mx8_forward(const Mx8Fwd& a, void* ws, hipStream_t st) {
     g.out8 = a.out8;
     g.pre8 = a.pre8;
     if (mx8_few_rows(a.M, a.x.ld)) {
-      hipLaunchKernelGGL((mx8_rows<T>), dim3((unsigned)ceil_div(a.N, 32)), dim3(1024), 0, st, g);
+      hipLaunchKernelGGL((mx8_rows<T>), dim3((unsigned)ceil_div(a.N, 32)), dim3(64 * kFewRowsWaves), 0, st, g);
       return hipGetLastError();
     }
     const Cut c = cut_mx8(a.M, a.N, a.x.ld, (int)sizeof(T));

@@ -657,13 +657,13 @@ __global__ void __launch_bounds__(512) mx8_gemm_tile256(Mx8Args<bf16> g) {
 //
 // Up to 16 rows (serving: single tokens), where the weights' bytes are all the time there is: the same matrix instructions on
 // operands straight from memory, each weight read once.  A workgroup takes 32 columns and 16 rows; its 16
-// waves take stages of 128 k's in turn, the loads of two under way, and their sums meet in the LDS, added in order.
-// 1 x 1,024 x 4,096 with GELU: 4.4 to 5.0 us for 4.3 MB, about 1 TB/s: the latency of two loads one after another (a
-// kernel's arguments, then the weights), the sums' meeting and the launch.
+// waves take a stage of 128 k's each, as far as there are, and their sums meet in the LDS, added in order.
+// 1 x 1,024 x 4,096 with GELU: 3.9 us for 4.3 MB in a graph of such calls, 1.1 TB/s (fp32 4.2): the latency of two loads one
+// after another (a kernel's arguments, then the weights), the sums' meeting and the launch.
 template <typename T>
-__global__ void __launch_bounds__(1024) mx8_rows(Mx8Args<T> g) {
+__global__ void __launch_bounds__(64 * kFewRowsWaves) mx8_rows(Mx8Args<T> g) {
   constexpr bool WIDE = sizeof(T) == 4;
-  constexpr int NW = 16, PF = 2;
+  constexpr int NW = kFewRowsWaves;
   __shared__ float sums[NW][512];
   const int lane = threadIdx.x & 63, gq = lane >> 4, l16 = lane & 15;
   const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
@@ -689,22 +689,11 @@ __global__ void __launch_bounds__(1024) mx8_rows(Mx8Args<T> g) {
   };
   auto scale = [&](const uint8_t* p, int64_t k) { return k / kBlock8 + gq < sld ? (int)p[k / kBlock8 + gq] : 127; };
   f32x4 acc[1][2] = {{f32x4{0.f, 0.f, 0.f, 0.f}, f32x4{0.f, 0.f, 0.f, 0.f}}};
-  for (int64_t k0 = 128 * wave; k0 < g.ld; k0 += 128 * NW * PF) {
-    Mx8Op fx[PF][1], fw[PF][2];
-    int cx[PF][1], cw[PF][2];
-#pragma unroll
-    for (int i = 0; i < PF; ++i) {
-      const int64_t k = k0 + 128 * NW * i;
-      fx[i][0] = operand(x, k);
-      cx[i][0] = scale(xs, k);
-#pragma unroll
-      for (int b = 0; b < 2; ++b) {
-        fw[i][b] = operand(w[b], k);
-        cw[i][b] = scale(ws[b], k);
-      }
-    }
-#pragma unroll
-    for (int i = 0; i < PF; ++i) mx8_products<T>(fx[i], fw[i], cx[i], cw[i], acc, 0);
+  const int64_t k = 128 * wave;
+  if (k < g.ld) {
+    const Mx8Op fx[1] = {operand(x, k)}, fw[2] = {operand(w[0], k), operand(w[1], k)};
+    const int cx[1] = {scale(xs, k)}, cw[2] = {scale(ws[0], k), scale(ws[1], k)};
+    mx8_products<T>(fx, fw, cx, cw, acc, 0);
   }
   const int64_t n = n0 + 8 * gq;
   float o[8], bias[8];

@@ -32,7 +32,8 @@ inline Cut cut_mx8(int64_t M, int64_t N, int64_t ld, int es) {
 }
 // Whether mx8_rows takes the product (with GELU, bf16: 1,024 x 4,096 4.4 us for one row, 4.9 for sixteen, where mx8_gemm_tile
 // takes 5.8 for either; 2,048 x 512, sixteen rows 6.8 and 7.8; but 4,096 x 1,024 10.6 and 8.9, one row 8.4 and 8.2).
-inline bool mx8_few_rows(int64_t M, int64_t ld) { return M <= 16 && ld <= 2048; }
+constexpr int kFewRowsWaves = 16;  // a workgroup's, a stage of 128 k's each
+inline bool mx8_few_rows(int64_t M, int64_t ld) { return M <= 16 && ld <= 128 * kFewRowsWaves; }
 inline size_t mx8_part_bytes(int64_t M, int64_t N, int64_t ld, int es) {
   return mx8_few_rows(M, ld) ? 0 : part_of(M, N, cut_mx8(M, N, ld, es));
 }
