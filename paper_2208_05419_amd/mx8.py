@@ -100,7 +100,7 @@ def _fit8(t, lead, C, device) -> bool:
     import torch
     if t is None:
         return True
-    if type(t) is not Mx8 or t.channels != C:
+    if type(t) is not Mx8 or t.channels != C or C < 1:
         return False
     values, scales, _ = t
     blocks = -(-C // BLOCK)
@@ -120,7 +120,9 @@ def _expect8(name, t, shape, device):
     values, scales, C = t
     if values.dtype != torch.float8_e4m3fn or scales.dtype != torch.float8_e8m0fnu:
         raise TypeError(f"{name} must have float8_e4m3fn values and float8_e8m0fnu scales")
-    if C != shape[-1] or C < 1:
+    if C < 1:
+        raise ValueError(f"{name} has no channels")
+    if C != shape[-1]:
         raise ValueError(f"{name} has {C} channels, expected {shape[-1]}")
     blocks = -(-C // BLOCK)
     if values.shape != (*shape[:-1], BLOCK * blocks) or scales.shape != (*shape[:-1], blocks):
