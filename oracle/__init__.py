@@ -29,7 +29,7 @@ def _load():
     if _lib is not None:
         return _lib
     if not os.path.exists(_LIB_PATH):
-        from . import build as _b  # the checker is C; build it on first use
+        from . import build as _b  # the oracle is C; build it on first use
         _b.build()
     lib = ctypes.CDLL(_LIB_PATH)
     lib.orc_keep_counts.argtypes = [_l, _l, ctypes.c_double, ctypes.POINTER(_l), ctypes.POINTER(_l)]

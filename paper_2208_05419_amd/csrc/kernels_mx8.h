@@ -15,7 +15,7 @@ namespace afno {
 
 // x [M][C] at any address to q, s.  One pass, bound by memory: eight neighbouring values a thread, a load of 16 bytes
 // (two in fp32), a block's largest value by two exchanges among its four threads (64,800 x 1,024 bf16: 41 us for 201 MB,
-// 4.9 TB/s, a copy's rate).
+// 4.9 TB/s, a copy's rate; fp32 59 us with one set of inputs, 5.7 TB/s).
 template <typename T>
 __global__ void __launch_bounds__(256) mx8_pack_kernel(const T* __restrict__ x, Rows8 o, int64_t M, int64_t C) {
   constexpr int UE = Unit<T>::UE, NU = 8 / UE;
@@ -39,7 +39,7 @@ __global__ void __launch_bounds__(256) mx8_pack_kernel(const T* __restrict__ x, 
 // The values that q, s stand for, eight to a thread, as rows of ldo values (C of them, zeros behind; ALIGNED: ldo a multiple
 // of 8 and out 16-byte aligned).  No rounding: the stored values are normal numbers of either type.  Bound by memory
 // (64,800 x 1,024 to bf16: 31 to 35 us for 201 MB, 5.7 to 6.5 TB/s, part of the eight bits from the caches; 64,800 x
-// 4,096 141 us, 5.7 TB/s).
+// 4,096 141 us, 5.7 TB/s; 64,800 x 1,024 to fp32 89 us, 3.8 TB/s, four fifths of it stores).
 template <typename T, bool ALIGNED>
 __global__ void __launch_bounds__(256) mx8_unpack_kernel(const uint8_t* __restrict__ q, const uint8_t* __restrict__ s,
                                                          int64_t ld, T* __restrict__ out, int64_t ldo, int64_t M) {
@@ -122,7 +122,8 @@ __device__ __forceinline__ void put8(const Rows8& o, int64_t m, int64_t c, const
 
 // C <= CAP: W waves a row, 4 / W rows a workgroup.  residual, out, sum and o.q may be null.  A row stays in registers
 // from its sum to its eight bits, so that everything is read and written once: bound by memory (64,800 x 1,024 bf16 with a
-// residual, its sum and eight bits: 91 us for 467 MB, 5.1 TB/s; one row 2.6 us, latency).
+// residual, its sum and eight bits: 91 us for 467 MB, 5.1 TB/s, fp32 149 us with one set of inputs, 5.8 TB/s; one row 2.7 us,
+// latency).
 template <typename T, bool VEC, int CAP, int W>
 __global__ void __launch_bounds__(256) rms_rows(const T* __restrict__ x, const T* __restrict__ residual,
                                                 const T* __restrict__ gamma, T* __restrict__ out,
@@ -178,8 +179,9 @@ __global__ void __launch_bounds__(256) rms_rows(const T* __restrict__ x, const T
 }
 
 // C <= CAP: as norm_rows_backward, rows shared by the grid's workgroups, the next row's loads under way during
-// the present one's sums; part [gridDim.x][C].  Bound by memory (64,800 x 1,024 bf16 with gsum: 96 us for 531 MB, 5.5 TB/s);
-// few odd rows (5,187 x 333 fp32: 9 us) by the latency of gamma's and a row's loads and its two sums.
+// the present one's sums; part [gridDim.x][C].  Bound by memory (64,800 x 1,024 bf16 with gsum: 95 us for 531 MB, 5.6 TB/s,
+// fp32 152 us with one set of inputs, part of it from the caches); few odd rows (5,187 x 333 fp32: 9 us) by the latency of
+// gamma's and a row's loads and its two sums.
 template <typename T, bool VEC, int CAP, int W>
 __global__ void __launch_bounds__(256) rms_rows_backward(const T* __restrict__ g, const T* __restrict__ x,
                                                          const T* __restrict__ gamma, const T* __restrict__ gsum,
@@ -276,7 +278,8 @@ __global__ void __launch_bounds__(256) rms_rows_backward(const T* __restrict__ g
 }
 
 // Rows of any width, a workgroup a row, read again for each pass (from the caches): 2,000 x 9,001 bf16
-// with a residual, its sum and eight bits 63 us for 127 MB, 2.0 TB/s: value by value, three passes.
+// with a residual, its sum and eight bits 63 us for 127 MB, 2.0 TB/s: value by value, three passes, since a row begins at any
+// address and a lane's values of one pass are no longer in registers in the next.
 template <typename T>
 __global__ void __launch_bounds__(256) rms_wide(const T* __restrict__ x, const T* __restrict__ residual,
                                                 const T* __restrict__ gamma, T* __restrict__ out,

@@ -88,12 +88,13 @@ struct Mx8Args {
 };
 
 // W rows of a stage's 128 k's as a slab in the LDS: rows of 128 bytes, the 16-byte chunk c of row r at place
-// c ^ f(r), so that the rows that a pass of ds_read_b128 takes cover the banks once.  A wave takes the WAVE rows
+// c ^ f(r), so that the rows that a pass of ds_read_b128 takes cover the banks once (WIDE: twice).  A wave takes the WAVE rows
 // from WAVE * its place.  B: the second operand, whose rows are dealt to the tiles of 16 so that in the
 // transposed product a lane ends up with NV = WAVE / 4 neighbouring columns (16, the 16 bytes of a store in eight bits,
 // or 8): tile b, lane l16 = 4 r + c has row NV r + 4 b + c.
 // WIDE: a lane's two chunks of a row are a block's, 2 gq and 2 gq + 1, and not gq and 4 + gq, so that one scale widens
-// both.
+// both.  Two lane groups' chunks then differ in bit 1 where gq's differ in bit 0, and rows of one parity meet on the same
+// banks: 0.43 conflicts an access are counted in fp32.
 template <bool B, bool WIDE, int W, int WAVE, int NT>
 struct Slab8 {
   static constexpr int CH = 8, U = W * CH, L = U / NT;  // chunks of a row, 16-byte units, loads a lane
@@ -201,9 +202,9 @@ struct Place8 {
 };
 
 // NV (8 or 16) neighbouring values from a place on, in eight bits; JOIN, which lanes have the rest of the
-// block: the next ones, the ones 16 apart, the one 32 apart.  All lanes of the wave together.  there: the row exists
+// block: the next ones or the ones 16 apart.  All lanes of the wave together.  there: the row exists
 // (columns behind the last are not stored).
-enum { kNeighbours, kRowsApart, kHalves };
+enum { kNeighbours, kRowsApart };
 template <int NV, int JOIN>
 __device__ __forceinline__ void store8(const Rows8& o, const Place8& p, int64_t N, const float (&z)[NV], bool there) {
   const int64_t n = p.n;
@@ -216,7 +217,7 @@ __device__ __forceinline__ void store8(const Rows8& o, const Place8& p, int64_t 
   }
   constexpr int LANES = kBlock8 / NV;
   const int byte = block_scale8(v, [](float top) {
-    return JOIN == kNeighbours ? lanes_max<LANES>(top) : JOIN == kRowsApart ? rows_max<LANES>(top) : halves_max(top);
+    return JOIN == kNeighbours ? lanes_max<LANES>(top) : rows_max<LANES>(top);
   });
   uint32_t w[NV / 4];
   round8(v, byte, w);
@@ -241,8 +242,10 @@ union Some {
 };
 
 // The epilogue of NV neighbouring values, their biases added; as store8 all lanes of the wave together.  In bf16 the
-// short GELU, whose error is below that of the eight-bit instruction (64,800 x 1,024 x 4,096 to eight bits: 473 us, 501 with
-// the other one).  The results in the storage type go out by ordinary stores (392 us; past the caches 442).
+// short GELU, whose error is below that of the eight-bit instruction (64,800 x 1,024 x 4,096 to eight bits: 422 us, 456 with
+// the other one, with dropout and both results 586 and 609; few rows and joined splits take it too, so that a product's
+// GELU is the same for any number of rows).  The results in the storage type go out by ordinary stores (392 us; past the
+// caches 442).
 template <typename T, int NV, int JOIN>
 __device__ __forceinline__ void finish8(const Mx8Args<T>& g, const Drop& d, const Place8& p, float (&o)[NV],
                                         bool units) {
@@ -378,7 +381,8 @@ __device__ __forceinline__ void mx8_store(const Mx8Args<T>& g, const Drop& d, co
 // took 769 us for 473 in tiles of 128.  Tiles of 128: 10,368 x 1,536 x 384 with GELU 17 us, 720 TFLOP/s, one tile of twelve
 // stages on nearly every CU: latency and the one epilogue.  In fp32: 64,800 x 1,024 x 1,024 220 us, 616 TFLOP/s, 16,200 x
 // 4,096 x 1,024 157 us, 867 (matrix cores 32 %), bound by the widening of each operand to bfloat16 in every wave that reads
-// it, half as often as in tiles of 64 (320 and 211 us).  Few rows: 64 x 4,096 x 1,024 in four splits 6.4 us, latency.
+// it, half as often as in tiles of 64 (320 and 211 us), and by the LDS reads for that, whose rows meet on banks (Slab8's WIDE).
+// Few rows: 64 x 4,096 x 1,024 in four splits 6.4 us, latency.
 template <typename T, int TILE>
 __global__ void __launch_bounds__(256, 2) mx8_gemm_tile(Mx8Args<T> g) {
   constexpr int NT = 256, WR = TILE / 2, TM = WR / 16, TN = WR / 16, NS = TILE == 128 ? 2 : 4;
@@ -521,8 +525,10 @@ __global__ void __launch_bounds__(256, 2) mx8_gemm_tile(Mx8Args<T> g) {
 // Workgroup tile 256 x 256 in bf16, 8 waves as 2 x 4 of 128 x 64, two LDS buffers of 64 KB, the two groups of waves
 // in turn at the LDS and the matrix cores as in gemm_tile256: a stage is four turns of two row tiles by four column tiles.
 // The scales of four stages lie in the LDS, 16 bytes to a row, which each thread loads for one row (in registers they
-// spill).  8,192 x 8,192 x 8,192 to eight bits: 433 us, 2,540 TFLOP/s, the matrix cores busy in 59 % of the cycles: four turns
-// of 8 products and the LDS reads for them.  64,800 x 4,096 x 1,024 261 us, 2,080 TFLOP/s; 64,800 x 1,024 x 4,096, eight
+// spill); of the second operand's, four rows that a wave reads lie 256 bytes apart, on the same banks (0.25 conflicts an
+// access are counted).  8,192 x 8,192 x 8,192 to eight bits: 433 us, 2,540 TFLOP/s, the matrix cores busy in 59 % of the
+// cycles: four turns of 8 products, of which the first waits for twelve reads of 16 bytes and all twelve scales, the others for
+// four reads.  64,800 x 4,096 x 1,024 261 us, 2,080 TFLOP/s; 64,800 x 1,024 x 4,096, eight
 // stages and an epilogue of 65,536 values, 392 us in bf16, 350 in eight bits, with GELU 420, with dropout and the value
 // before GELU in eight bits 591 to 615 (matrix cores 19 %, vector ALUs 44 %): one workgroup a CU, whose epilogue leaves the
 // matrix cores idle.  Workgroups that stay, with the next tile's first loads under way during the epilogue: 457 us for 392,
@@ -658,7 +664,7 @@ __global__ void __launch_bounds__(512) mx8_gemm_tile256(Mx8Args<bf16> g) {
 // Up to 16 rows (serving: single tokens), where the weights' bytes are all the time there is: the same matrix instructions on
 // operands straight from memory, each weight read once.  A workgroup takes 32 columns and 16 rows; its 16
 // waves take a stage of 128 k's each, as far as there are, and their sums meet in the LDS, added in order.
-// 1 x 1,024 x 4,096 with GELU: 3.9 us for 4.3 MB in a graph of such calls, 1.1 TB/s (fp32 4.2): the latency of two loads one
+// 1 x 1,024 x 4,096 with GELU: 3.9 us for 4.3 MB in a graph of a hundred such calls, 1.1 TB/s (fp32 4.2): the latency of two loads one
 // after another (a kernel's arguments, then the weights), the sums' meeting and the launch.
 template <typename T>
 __global__ void __launch_bounds__(64 * kFewRowsWaves) mx8_rows(Mx8Args<T> g) {
